@@ -233,7 +233,94 @@ rv_status rv_fuse_accept_noalloc(const float* d_logits, int32_t batch, int32_t k
                                  const int32_t* d_draft_ids, const rv_fusion* fusion, int32_t* d_accept_len,
                                  int32_t* d_next_id, void* stream);
 
+/* ---- operators on the cache ----
+ *
+ * For programs that keep several continuations of one prompt, or that compute
+ * their own projections: rows are written to a layer of the cache, sequences are
+ * copied or forked, and query rows attend a layer.  rv_verify* on a forked cache
+ * attends the same way.
+ *
+ * A call on rows takes two host arrays: sequence b has h_rows[b] rows (0 for
+ * none) at positions h_pos[b] .. h_pos[b] + h_rows[b] - 1, all below max_len
+ * (else RV_E_RANGE); the rows of the batch follow each other, sequence after
+ * sequence.  A row is n heads x head_dim values of RV_F32 or RV_BF16, whatever
+ * the model's type; rows start at multiples of 16 bytes, `ld` elements apart.
+ * Calls on one cache share its workspace and its tables: they, and graphs that
+ * hold them, must not overlap (as for rv_verify).  Host arrays are read before
+ * the call returns; a captured call keeps the values it was captured with, also
+ * those of the cache's tiles, so a graph is captured anew after a fork, a copy or
+ * a prefill that changes which tiles are shared. */
+
+typedef struct {
+  int32_t dtype;                      /* of all rows: RV_F32 or RV_BF16 */
+  int32_t rotate;                     /* 0: keys (and queries) are stored as they are */
+  const void *d_q, *d_k, *d_v;        /* n_heads, n_kv_heads, n_kv_heads heads; d_q may be NULL */
+  int64_t ld_q, ld_k, ld_v;
+  void* d_q_out;                      /* queries, normalised and rotated; may be d_q; NULL with d_q */
+  int64_t ld_q_out;
+  const float *d_q_gain, *d_k_gain;   /* [head_dim] fp32, or NULL: that side is not normalised */
+} rv_rows;
+
+/* What the rows of a call must fit: h_dims[0..3] = batch, n_heads, n_kv_heads, head_dim. */
+rv_status rv_cache_dims(const rv_cache* c, int32_t* h_dims);
+
+/* Writes rows of K and V to one layer of the cache.  With gains, each head x of
+ * a query or key is first normalised, y = x / sqrt(mean(x^2) + rms_eps) * g;
+ * with `rotate` queries and keys are rotated to their positions (rotate-half, as
+ * in the pass).  Rows of the sequence at other positions stay as they are, and so
+ * does the id history.  RV_E_STATE for positions of a tile that another sequence
+ * shares (rv_cache_fork).  Asynchronous. */
+rv_status rv_cache_append(rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows,
+                          const rv_rows* rows, void* stream);
+
+/* Reads K and V rows of one layer back as values (hi + lo for bf16 models). */
+rv_status rv_cache_read(const rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows, int32_t dtype,
+                        void* d_k, int64_t ld_k, void* d_v, int64_t ld_v, void* stream);
+
+/* Copies sequences: h_dst[i] becomes what h_src[i] was before the call, up to
+ * its first h_len[i] committed tokens: ids 0 .. len-1 and, in every layer, K and
+ * V of positions 0 .. len-2 (what later positions of the last 64 hold is
+ * unspecified).  All moves read before any of them writes, so sequences may
+ * change places; destinations are distinct.  A destination shares no tiles
+ * afterwards (h_dst[i] == h_src[i] gives a forked sequence its own copy).
+ * RV_E_STATE if a sequence that the call does not overwrite shares tiles of a
+ * destination.  1 <= len <= max_len.  Asynchronous. */
+rv_status rv_cache_copy(rv_cache* c, int32_t n, const int32_t* h_src, const int32_t* h_dst, const int32_t* h_len,
+                        void* stream);
+
+/* The n sequences h_dst (distinct, not src) continue the first `len` committed
+ * tokens of src: ids 0 .. len-1 and K and V of positions 0 .. len-2.  Whole tiles
+ * of 64 positions below len - 1 are not copied: the forks read them where src
+ * does.  None of the sequences that read a tile can write to it any more (calls
+ * that would return RV_E_STATE), until they stop sharing it: a sequence does when
+ * rv_cache_copy or rv_cache_fork writes it, all do at rv_prefill_cache.
+ * RV_E_STATE if a sequence that the call does not overwrite shares tiles of a
+ * destination.  Asynchronous. */
+rv_status rv_cache_fork(rv_cache* c, int32_t src, int32_t len, int32_t n, const int32_t* h_dst, void* stream);
+
+/* Attention of query rows against one layer: a row at position p of sequence b
+ * attends positions 0 .. p of b.  Queries are taken as they are (rotated; scaled
+ * by 1 / sqrt(head_dim) here), query head h with kv head h / (n_heads /
+ * n_kv_heads).  Tiles that several sequences of the call share are read once for
+ * all their rows.  At most as many rows as the workspace holds: max(batch *
+ * max_block, 2048) (else RV_E_CAPACITY).  d_out may be d_q.  Asynchronous. */
+rv_status rv_cache_attend(const rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows, int32_t dtype,
+                          const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* stream);
+
+/* From now on the passes of this model normalise queries and keys for each head
+ * before the rotation (as rv_cache_append does), with gains [n_layers][head_dim]
+ * fp32 in the caller's device memory (at multiples of 16 bytes, kept for as long
+ * as the model runs); NULL for both: no norms, as after rv_init_weights. */
+rv_status rv_model_qk_norm(rv_model* m, const float* d_q_gain, const float* d_k_gain);
+
 /* ---- inspection (tests and benchmarks) ---- */
+
+/* Where a part of the cache lies in the caller's buffer (bytes): K or V of every
+ * layer [layer][b][kv_head] x (max_len rounded up to a multiple of 64) x head_dim
+ * (fp32, or the bf16 hi plane; the low planes of bf16 models), or the id history
+ * [b][max_len].  Tiles of 64 positions are contiguous in it. */
+enum { RV_SPAN_K = 0, RV_SPAN_V = 1, RV_SPAN_K_LO = 2, RV_SPAN_V_LO = 3, RV_SPAN_IDS = 4 };
+rv_status rv_debug_cache_span(const rv_cache* c, int32_t which, size_t* offset, size_t* bytes);
 
 /* The fusion, log-softmax and accept stage of rv_verify (Eq. 2; Algorithm 2,
  * or Algorithm 3 with RV_RULE_TYPICAL; Appendix A) run by the same kernels

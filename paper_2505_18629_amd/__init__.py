@@ -35,6 +35,7 @@ RV_MAX_BATCH, RV_MAX_DRAFTS = 256, 32
  RV_OUT_MARGINS, RV_OUT_PROB_FUSED) = range(9)
 RV_MAT_QKV, RV_MAT_O, RV_MAT_GATEUP, RV_MAT_DOWN, RV_MAT_LM_HEAD = range(5)
 RV_WS_RESID, RV_WS_ATTN, RV_WS_ACT, RV_WS_QUERY = range(4)
+RV_SPAN_K, RV_SPAN_V, RV_SPAN_K_LO, RV_SPAN_V_LO, RV_SPAN_IDS = range(5)
 PROF_CLASSES = ["plan", "norm", "qkv", "attn", "combine", "o", "gateup", "down", "lmhead", "tail"]
 STATUS = {0: "RV_OK", -1: "RV_E_ARG", -2: "RV_E_RANGE", -3: "RV_E_CAPACITY", -4: "RV_E_BUFFER",
           -5: "RV_E_HIP", -6: "RV_E_STATE"}
@@ -43,9 +44,11 @@ EXPORTED = [
     "rv_status_str", "rv_last_error", "rv_model_bytes", "rv_init_weights", "rv_model_free",
     "rv_cache_bytes", "rv_cache_create", "rv_cache_free", "rv_prefill_cache", "rv_verify", "rv_verify_sampled",
     "rv_verify_ragged", "rv_commit_tokens", "rv_fuse_accept_noalloc",
+    "rv_cache_append", "rv_cache_read", "rv_cache_copy", "rv_cache_fork", "rv_cache_attend", "rv_cache_dims",
+    "rv_model_qk_norm",
     "rv_debug_fuse_accept", "rv_debug_output", "rv_debug_export_kv", "rv_debug_export_ids", "rv_debug_weight_bits",
     "rv_debug_linear", "rv_debug_workspace", "rv_debug_profile", "rv_debug_profile_read", "rv_debug_time_matrix",
-    "rv_debug_force_matmul",
+    "rv_debug_force_matmul", "rv_debug_cache_span",
 ]
 
 
@@ -62,6 +65,13 @@ class rv_fusion(ctypes.Structure):
                 ("temperature", ctypes.c_float)]
 
 
+class rv_rows(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("rotate", ctypes.c_int32), ("d_q", ctypes.c_void_p),
+                ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
+                ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("d_q_out", ctypes.c_void_p),
+                ("ld_q_out", ctypes.c_int64), ("d_q_gain", ctypes.c_void_p), ("d_k_gain", ctypes.c_void_p)]
+
+
 class RVError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS.get(status, status)}: {message}")
@@ -69,7 +79,7 @@ class RVError(RuntimeError):
         self.name = STATUS.get(status, str(status))
 
 
-_vp, _i32, _u64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
+_vp, _i32, _i64, _u64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
 _P_i32 = ctypes.POINTER(ctypes.c_int32)
 _sig = {
     "rv_status_str": ([ctypes.c_int], ctypes.c_char_p),
@@ -88,6 +98,14 @@ _sig = {
     "rv_verify_ragged": ([_vp, _P_i32, _vp, _i32, _P_i32, _vp, _i32, ctypes.POINTER(rv_fusion), _vp, _vp, _vp],
                          ctypes.c_int),
     "rv_fuse_accept_noalloc": ([_vp, _i32, _i32, _i32, _vp, ctypes.POINTER(rv_fusion), _vp, _vp, _vp], ctypes.c_int),
+    "rv_cache_append": ([_vp, _i32, _vp, _vp, ctypes.POINTER(rv_rows), _vp], ctypes.c_int),
+    "rv_cache_read": ([_vp, _i32, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
+    "rv_cache_copy": ([_vp, _i32, _vp, _vp, _vp, _vp], ctypes.c_int),
+    "rv_cache_fork": ([_vp, _i32, _i32, _i32, _vp, _vp], ctypes.c_int),
+    "rv_cache_attend": ([_vp, _i32, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
+    "rv_cache_dims": ([_vp, _vp], ctypes.c_int),
+    "rv_model_qk_norm": ([_vp, _vp, _vp], ctypes.c_int),
+    "rv_debug_cache_span": ([_vp, _i32, ctypes.POINTER(_sz), ctypes.POINTER(_sz)], ctypes.c_int),
     "rv_debug_fuse_accept": ([_vp, _vp, _P_i32, _vp, _i32, ctypes.POINTER(rv_fusion), _vp, _vp, _vp], ctypes.c_int),
     "rv_debug_output": ([_vp, _i32, _vp, _sz, _vp], ctypes.c_int),
     "rv_debug_export_kv": ([_vp, _i32, _i32, _i32, _i32, _vp, _vp, _sz, _vp], ctypes.c_int),
@@ -237,6 +255,111 @@ def rv_fuse_accept_noalloc(logits, k: int, draft_ids, alpha: float, accept_len, 
                                        ctypes.byref(fu), _dev(accept_len), _dev(next_id), _stream(stream)))
 
 
+# operators on the cache: `positions` and `counts` are host arrays with an entry
+# per sequence; rows are 2-D tensors [rows][heads * head_dim], the sequences' rows
+# after each other, of which the second dimension is dense
+
+_ROW_TYPES = {torch.float32: RV_F32, torch.bfloat16: RV_BF16}
+
+
+def _i32_array(vals, n: Optional[int] = None) -> np.ndarray:
+    arr = np.ascontiguousarray(vals, dtype=np.int32)
+    if arr.ndim != 1 or (n is not None and arr.size != n):
+        raise ValueError(f"expected {'a list' if n is None else n} of whole numbers, got shape {arr.shape}")
+    return arr
+
+
+def _addr(arr: np.ndarray) -> int:
+    return arr.__array_interface__["data"][0]
+
+
+def rv_cache_dims(cache: int):
+    """(batch, query heads, kv heads, head_dim) of a cache and its model."""
+    d = (_i32 * 4)()
+    _check(_lib.rv_cache_dims(cache, d))
+    return tuple(d)
+
+
+def _spans(batch: int, positions, counts):
+    pos, n = _i32_array(positions, batch), _i32_array(counts, batch)
+    return pos, n, int(n.sum())
+
+
+def _row_type(total: int, *rows) -> int:
+    """Type of the rows; each (tensor, width) given holds `total` rows of one type on the current device."""
+    dtype, here = rows[0][0].dtype, torch.cuda.current_device()
+    if dtype not in _ROW_TYPES:
+        raise ValueError(f"rows must be float32 or bfloat16, not {dtype}")
+    for t, width in rows:
+        if tuple(t.shape) != (total, width) or t.dtype != dtype or (total and t.stride(1) != 1):
+            raise ValueError(f"expected {total} rows of {width} {dtype}, dense within a row, got {tuple(t.shape)} of "
+                             f"{t.dtype} with strides {t.stride()}")
+        if not t.is_cuda or t.device.index != here:
+            raise ValueError(f"rows on {t.device}, the current device is cuda:{here}")
+    return _ROW_TYPES[dtype]
+
+
+def _gain(t, shape) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"gains must be contiguous float32 {shape}, got {tuple(t.shape)} of {t.dtype}")
+    return _dev(t)
+
+
+def rv_cache_append(cache: int, layer: int, positions, counts, q, k, v, q_out, q_gain=None, k_gain=None,
+                    rotate: bool = True, stream=None) -> None:
+    """q and q_out may be None together; q_out may be q."""
+    batch, hq, hkv, hd = rv_cache_dims(cache)
+    pos, n, total = _spans(batch, positions, counts)
+    rows = [(k, hkv * hd), (v, hkv * hd)] + [(t, hq * hd) for t in (q, q_out) if t is not None]
+    kind = _row_type(total, *rows)
+    a = rv_rows(kind, 1 if rotate else 0, _dev(q), _dev(k), _dev(v), 0 if q is None else q.stride(0), k.stride(0),
+                v.stride(0), _dev(q_out), 0 if q_out is None else q_out.stride(0), _gain(q_gain, (hd,)),
+                _gain(k_gain, (hd,)))
+    _check(_lib.rv_cache_append(cache, layer, _addr(pos), _addr(n), ctypes.byref(a), _stream(stream)))
+
+
+def rv_cache_read(cache: int, layer: int, positions, counts, k, v, stream=None) -> None:
+    batch, _, hkv, hd = rv_cache_dims(cache)
+    pos, n, total = _spans(batch, positions, counts)
+    kind = _row_type(total, (k, hkv * hd), (v, hkv * hd))
+    _check(_lib.rv_cache_read(cache, layer, _addr(pos), _addr(n), kind, _dev(k), k.stride(0), _dev(v), v.stride(0),
+                              _stream(stream)))
+
+
+def rv_cache_copy(cache: int, src, dst, lengths, stream=None) -> None:
+    s = _i32_array(src)
+    d, n = _i32_array(dst, s.size), _i32_array(lengths, s.size)
+    _check(_lib.rv_cache_copy(cache, s.size, _addr(s), _addr(d), _addr(n), _stream(stream)))
+
+
+def rv_cache_fork(cache: int, src: int, length: int, dst, stream=None) -> None:
+    d = _i32_array(dst)
+    _check(_lib.rv_cache_fork(cache, src, length, d.size, _addr(d), _stream(stream)))
+
+
+def rv_cache_attend(cache: int, layer: int, positions, counts, q, out, stream=None) -> None:
+    """out may be q."""
+    batch, hq, _, hd = rv_cache_dims(cache)
+    pos, n, total = _spans(batch, positions, counts)
+    kind = _row_type(total, (q, hq * hd), (out, hq * hd))
+    _check(_lib.rv_cache_attend(cache, layer, _addr(pos), _addr(n), kind, _dev(q), q.stride(0), _dev(out),
+                                out.stride(0), _stream(stream)))
+
+
+def rv_model_qk_norm(model: int, q_gain, k_gain) -> None:
+    """q_gain, k_gain: device float32 [n_layers][head_dim], kept by the caller; None for both: no norms."""
+    _check(_lib.rv_model_qk_norm(model, _dev(q_gain), _dev(k_gain)))
+
+
+def rv_debug_cache_span(cache: int, which: int):
+    """(offset, bytes) of a part of the cache in its buffer."""
+    at, n = _sz(), _sz()
+    _check(_lib.rv_debug_cache_span(cache, which, ctypes.byref(at), ctypes.byref(n)))
+    return at.value, n.value
+
+
 def rv_debug_fuse_accept(cache: int, logits, prefix_len: Sequence[int], draft_ids, k: int, alpha: float,
                          accept_len, next_id, rule: int = RV_RULE_GREEDY, epsilon: float = 0.09, delta: float = 0.3,
                          entropy_src: int = RV_ENTROPY_FUSED, temperature: float = 1.0, stream=None) -> None:
@@ -335,6 +458,13 @@ class Verifier:
         rv_prefill_cache(self.cache, d_ids, lens)
         self._keep = d_ids
         return lens
+
+    def prefill_shared(self, prefix: Sequence[int]):
+        """All sequences continue one prompt: it is computed in the first and the others are forked from it."""
+        self.prefill([prefix] + [[0]] * (self.batch - 1))
+        if self.batch > 1:
+            rv_cache_fork(self.cache, 0, len(prefix), np.arange(1, self.batch, dtype=np.int32))
+        return [len(prefix)] * self.batch
 
     def verify_ragged(self, prefix_len, drafts: Sequence[Sequence[int]], probe, alpha: float, prefix_pos: int,
                       **kw):

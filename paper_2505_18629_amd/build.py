@@ -13,7 +13,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librv.so")
 
 WIDE = [f"k_wide_{e}.hip" for e in ("store", "resid", "partial", "swiglu", "qkv", "store_logical")]
-SOURCES = WIDE + ["k_init.hip", "k_gemm.hip", "k_attn.hip", "k_misc.hip", "k_head.hip", "rv_noalloc.hip", "rv_api.cpp"]
+SOURCES = WIDE + ["k_init.hip", "k_gemm.hip", "k_attn.hip", "k_misc.hip", "k_head.hip", "k_cache.hip", "k_share.hip",
+                  "rv_noalloc.hip", "rv_cache_ops.cpp", "rv_api.cpp"]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

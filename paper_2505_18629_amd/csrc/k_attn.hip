@@ -696,11 +696,11 @@ __global__ __launch_bounds__(256) void k_attn_combine(AttnArgs a, int hd) {
     put_operand4<DT>(a.out, a.out2, row, head * hd + 64 + 4 * (lane - 16), qd, x);
 }
 
-// Row-major copy of cached positions: one thread per (plane, head, position,
-// dim) element.
+// Row-major copy of cached positions into positions done.. of a destination of
+// dst_npos: one thread per (plane, head, position, dim) element.
 __global__ __launch_bounds__(256) void k_export_kv(const uint16_t* __restrict__ hi, const uint16_t* __restrict__ lo,
                                                    int hd, int n_kv, int kv_len, int pos0, int npos, bool is_v,
-                                                   uint16_t* __restrict__ dst) {
+                                                   uint16_t* __restrict__ dst, int dst_npos, int done) {
   const size_t per_plane = (size_t)n_kv * npos * hd;
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= 2 * per_plane) return;
@@ -708,17 +708,17 @@ __global__ __launch_bounds__(256) void k_export_kv(const uint16_t* __restrict__ 
   const size_t r = i % per_plane;
   const int head = (int)(r / ((size_t)npos * hd)), p = (int)(r / hd % npos), d = (int)(r % hd);
   const size_t src = (size_t)head * kv_len * hd + (is_v ? v_elem(pos0 + p, d, hd) : k_elem(pos0 + p, d, hd));
-  dst[i] = (pl ? lo : hi)[src];
+  dst[(((size_t)pl * n_kv + head) * dst_npos + done + p) * hd + d] = (pl ? lo : hi)[src];
 }
 
 }  // namespace
 
 hipError_t launch_export_kv(const void* src_hi, const void* src_lo, int hd, int n_kv, int kv_len, int pos0,
-                            int npos, bool is_v, void* dst, hipStream_t st) {
+                            int npos, bool is_v, void* dst, int dst_npos, int done, hipStream_t st) {
   const size_t n = (size_t)2 * n_kv * npos * hd;
   if (n == 0) return hipSuccess;
   k_export_kv<<<(unsigned)((n + 255) / 256), 256, 0, st>>>((const uint16_t*)src_hi, (const uint16_t*)src_lo, hd, n_kv,
-                                                           kv_len, pos0, npos, is_v, (uint16_t*)dst);
+                                                           kv_len, pos0, npos, is_v, (uint16_t*)dst, dst_npos, done);
   return hipGetLastError();
 }
 

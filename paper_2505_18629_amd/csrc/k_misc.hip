@@ -80,16 +80,19 @@ __global__ __launch_bounds__(1024) void k_rmsnorm(float* __restrict__ h, int d, 
 // writes the q operand or the K/V cache rows.  The first PB k-groups' loads
 // are issued before the token's position is read (they do not depend on
 // it), so the rotary table loads are the only dependent round trip.
-template <int DT, int PB>
-RV_DEV void qkv_finish_unit(const QkvFinish& a, int tok, int tile, int r0) {
+// NORM: q and k heads take their norm first (y = x / sqrt(mean(x^2) + eps) * g);
+// the hd / 8 units of a head are neighbouring lanes of one wave.
+template <int DT, int PB, bool NORM>
+RV_DEV void qkv_finish_unit(const QkvFinish& a, int row, int tile, int r0) {
   const int p0 = tile * 16;
-  auto part = [&](int g) { return a.P + ((size_t)g * a.M + tok) * a.N + p0; };
+  const int tok = row + a.tok0;
+  auto part = [&](int g) { return a.P + ((size_t)g * a.M + row) * a.N + p0; };
   f32x4_t l1[PB], l2[PB];
 #pragma unroll
   for (int v = 0; v < PB; ++v) {
-    const float* row = part(min(v, a.gk - 1));
-    l1[v] = *(const f32x4_t*)(row + r0);
-    l2[v] = *(const f32x4_t*)(row + 8 + r0);
+    const float* src = part(min(v, a.gk - 1));
+    l1[v] = *(const f32x4_t*)(src + r0);
+    l2[v] = *(const f32x4_t*)(src + 8 + r0);
   }
   const int pos = a.row_pos[tok], b = a.row_seq[tok];
   f32x4_t x1 = {0.f, 0.f, 0.f, 0.f}, x2 = {0.f, 0.f, 0.f, 0.f};
@@ -104,9 +107,9 @@ RV_DEV void qkv_finish_unit(const QkvFinish& a, int tok, int tile, int r0) {
     f32x4_t m1[8], m2[8];
 #pragma unroll
     for (int v = 0; v < 8; ++v) {
-      const float* row = part(min(g0 + v, a.gk - 1));
-      m1[v] = *(const f32x4_t*)(row + r0);
-      m2[v] = *(const f32x4_t*)(row + 8 + r0);
+      const float* src = part(min(g0 + v, a.gk - 1));
+      m1[v] = *(const f32x4_t*)(src + r0);
+      m2[v] = *(const f32x4_t*)(src + 8 + r0);
     }
 #pragma unroll
     for (int v = 0; v < 8; ++v) {
@@ -121,6 +124,16 @@ RV_DEV void qkv_finish_unit(const QkvFinish& a, int tok, int tile, int r0) {
     const bool is_q = p0 < a.q_rows;
     const int rel = is_q ? p0 : p0 - a.q_rows;
     const int head = rel / a.hd, j = (rel % a.hd) >> 4;
+    if constexpr (NORM) {
+      float ss = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ss += x1[i] * x1[i] + x2[i] * x2[i];
+      for (int m = 1; m < a.hd / 8; m *= 2) ss += __shfl_xor(ss, m, 64);
+      const float rs = 1.0f / sqrtf(ss / (float)a.hd + a.eps);
+      const float* gain = (is_q ? a.q_gain : a.k_gain) + 8 * j + r0;
+      x1 = x1 * rs * *(const f32x4_t*)gain;
+      x2 = x2 * rs * *(const f32x4_t*)(gain + half);
+    }
     const f32x4_t cs = *(const f32x4_t*)(a.rope_cos + (size_t)pos * half + 8 * j + r0);
     const f32x4_t sn = *(const f32x4_t*)(a.rope_sin + (size_t)pos * half + 8 * j + r0);
     f32x4_t o1, o2;
@@ -152,13 +165,13 @@ RV_DEV void qkv_finish_unit(const QkvFinish& a, int tok, int tile, int r0) {
 // q and k, and writes the q operand and the K/V cache rows.  Workgroups of
 // 256 threads, gridDim.y of them per token; a thread handles rows r0..r0+3
 // of a 16-row tile and their rotary partners r0+8..r0+11 (r0 in {0, 4}).
-template <int DT, int PB>
+template <int DT, int PB, bool NORM>
 __global__ __launch_bounds__(256) void k_qkv_finish(QkvFinish a) {
   const int tok = xcd_row(blockIdx.x, a.M);
   if (tok >= a.M) return;
   const int units = a.N / 8;
   for (int u = blockIdx.y * blockDim.x + threadIdx.x; u < units; u += gridDim.y * blockDim.x)
-    qkv_finish_unit<DT, PB>(a, tok, u >> 1, (u & 1) * 4);
+    qkv_finish_unit<DT, PB, NORM>(a, tok, u >> 1, (u & 1) * 4);
 }
 
 // Row-major [rows][K] <-> operand tiles, one element per thread.
@@ -310,7 +323,11 @@ hipError_t launch_qkv_finish(int dtype, const QkvFinish& a, hipStream_t st) {
   const int units = a.N / 8;
   const dim3 grid(xcd_grid(a.M), (units + 255) / 256);
   const int pb = a.gk <= 2 ? 2 : a.gk <= 4 ? 4 : 8;
-#define RV_FIN(DT_, PB_) k_qkv_finish<DT_, PB_><<<grid, 256, 0, st>>>(a)
+#define RV_FIN(DT_, PB_)                                              \
+  do {                                                                \
+    if (a.q_gain) k_qkv_finish<DT_, PB_, true><<<grid, 256, 0, st>>>(a); \
+    else k_qkv_finish<DT_, PB_, false><<<grid, 256, 0, st>>>(a);      \
+  } while (0)
   if (dtype == RV_BF16) {
     if (pb == 2) RV_FIN(RV_BF16, 2); else if (pb == 4) RV_FIN(RV_BF16, 4); else RV_FIN(RV_BF16, 8);
   } else {

@@ -1,0 +1,687 @@
+// Attention of query rows over a K/V cache in which sequences may share tiles.
+//
+// Row at position p of sequence b attends positions 0..p of b:
+//   out = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m),  s_j = q.k_j log2(e)/sqrt(hd).
+// Tiles that the sequences of a group all read (rv_cache_fork) lie before every
+// row of the group, so the queries of all its rows attend them together, without
+// a mask, and each tile is read once instead of once per sequence; each
+// sequence then attends the rest of its keys by itself, causally.  Runs of keys
+// of both parts leave unnormalised partial results, which the last kernel merges
+// in a fixed order (shared runs, then own).
+#include "rv_internal.h"
+
+namespace {
+
+constexpr int kKB = kTile;
+
+// What one workgroup attends: keys [kbeg, kend) as table row `seq` reads them,
+// by queries q_begin.. of nq (query slots of one kv head).
+struct Unit {
+  int seq, kbeg, kend, nq, q_begin, slot, kvh;
+  int first, rmax, tiles;  // group: its first member, rows per member; own part: first = -1
+};
+
+// Query slot q of a unit: its row, head and the last key it may see.
+struct Query {
+  bool valid;
+  int row, head, last;
+};
+
+template <int PART>
+RV_DEV bool unit_of(const ShareArgs& a, int x, Unit& u) {
+  const SharePart& sp = PART ? a.p.own : a.p.sh;
+  // query groups of one (run, sequence, kv head) are 8 workgroups apart: the
+  // same XCD, whose L2 then holds their tiles
+  const int j = x / 8, per = j / sp.nqg, qg = j % sp.nqg;
+  int i = per * 8 + x % 8;
+  const int run = i % sp.ns;
+  i /= sp.ns;
+  u.kvh = i % a.n_kv;
+  i /= a.n_kv;
+  const int G = a.n_heads / a.n_kv;
+  if (PART) {
+    if (i >= a.p.nseq) return false;
+    const int n = a.row0[i + 1] - a.row0[i], g = a.p.group_of[i];
+    const int k0 = g == 255 ? 0 : a.p.tiles[g] * kKB;
+    u.seq = i;
+    u.first = -1;
+    u.rmax = 0;
+    u.nq = n * G;
+    u.q_begin = qg * sp.qpw;
+    if (u.q_begin >= u.nq) return false;
+    const int q_last = min(u.nq, u.q_begin + sp.qpw) - 1;
+    u.kbeg = k0 + run * sp.ks;
+    u.kend = min(a.pos0[i] + q_last / G + 1, u.kbeg + sp.ks);
+    u.slot = (a.p.groups ? a.p.sh.ns : 0) + run;
+  } else {
+    if (i >= a.p.groups) return false;
+    u.first = a.p.first[i];
+    u.rmax = a.p.rmax[i];
+    u.seq = a.p.member[u.first];
+    u.nq = (a.p.first[i + 1] - u.first) * u.rmax * G;
+    u.q_begin = qg * sp.qpw;
+    if (u.q_begin >= u.nq) return false;
+    u.kbeg = run * sp.ks;
+    u.kend = min(a.p.tiles[i] * kKB, u.kbeg + sp.ks);
+    u.slot = run;
+  }
+  return u.kbeg < u.kend;
+}
+
+template <int PART>
+RV_DEV Query query_of(const ShareArgs& a, const Unit& u, int q) {
+  const int G = a.n_heads / a.n_kv;
+  Query r;
+  const int qc = min(q, u.nq - 1);
+  r.head = u.kvh * G + qc % G;
+  if (PART) {
+    r.valid = q < u.nq;
+    r.row = a.row0[u.seq] + qc / G;
+    r.last = a.pos0[u.seq] + qc / G;
+  } else {
+    const int i = qc / G, m = i / u.rmax, seq = a.p.member[u.first + m], n = a.row0[seq + 1] - a.row0[seq];
+    const int k = i - m * u.rmax;
+    r.valid = q < u.nq && k < n;
+    r.row = a.row0[seq] + min(k, n - 1);
+    r.last = 0x7fffffff;
+  }
+  return r;
+}
+
+// The last key that every query of a unit sees.
+template <int PART>
+RV_DEV int first_limit(const ShareArgs& a, const Unit& u) {
+  return PART ? a.pos0[u.seq] + u.q_begin / (a.n_heads / a.n_kv) : 0x7fffffff;
+}
+
+// First element of tile t of (table row seq, kv head) in a plane of this layer.
+template <int HD>
+RV_DEV size_t tile_base(const ShareArgs& a, int seq, int kvh, int t) {
+  const int slot = a.own ? __builtin_amdgcn_readfirstlane(a.own[(size_t)seq * (a.kv_len / kKB) + t]) : seq;
+  return ((size_t)(slot * a.n_kv + kvh) * a.kv_len + (size_t)t * kKB) * HD;
+}
+
+// B operands of one query: dims 32c + 8g .. +7 of chunk c as hi and lo planes.
+template <int HD>
+RV_DEV void load_query(const ShareArgs& a, const Query& q, int g, u32x4 (&hi)[HD / 32], u32x4 (&lo)[HD / 32]) {
+#pragma unroll
+  for (int c = 0; c < HD / 32; ++c) {
+    const int d = q.head * HD + 32 * c + 8 * g;
+    if (a.q_kind == ROWS_OPERAND) {
+      const size_t o = operand_offset(q.row, d, a.n_heads * HD, 2);
+      hi[c] = *(const u32x4*)((const char*)a.q + o);
+      lo[c] = *(const u32x4*)((const char*)a.q2 + o);
+    } else if (a.q_kind == RV_BF16) {
+      hi[c] = *(const u32x4*)((const uint16_t*)a.q + (size_t)q.row * a.ldq + d);
+      lo[c] = u32x4{0, 0, 0, 0};
+    } else {
+      const float* p = (const float*)a.q + (size_t)q.row * a.ldq + d;
+      const f32x4_t x = *(const f32x4_t*)p, y = *(const f32x4_t*)(p + 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = j < 2 ? x[2 * j] : y[2 * j - 4], f = j < 2 ? x[2 * j + 1] : y[2 * j - 3];
+        const uint16_t eh = f2bf(e), fh = f2bf(f);
+        hi[c][j] = eh | (uint32_t)fh << 16;
+        lo[c][j] = f2bf(e - bf2f(eh)) | (uint32_t)f2bf(f - bf2f(fh)) << 16;
+      }
+    }
+  }
+}
+
+// 4 consecutive dims of a row's head in the output's form.
+template <int DT>
+RV_DEV void put_out4(const ShareArgs& a, int hd, int row, int head, int d, const f32x4_t& x) {
+  const int k = head * hd + d;
+  if (a.o_kind == ROWS_OPERAND) {
+    put_operand4<DT>(a.out, a.out2, row, k, a.n_heads * hd, x);
+  } else if (a.o_kind == RV_BF16) {
+    uint16_t h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = f2bf(x[j]);
+    memcpy((uint16_t*)a.out + (size_t)row * a.ldo + k, h, 8);
+  } else {
+    *(f32x4_t*)((float*)a.out + (size_t)row * a.ldo + k) = x;
+  }
+}
+
+RV_DEV size_t part_index(const ShareArgs& a, int slot, int row, int head) {
+  return ((size_t)slot * a.p.rows + row) * a.n_heads + head;
+}
+
+// Softmax weights of one query's scores of NB 16-key blocks: masks keys past
+// the limit, folds them into (m, l) and leaves 2^(s - m) in s.  Returns the
+// factor for what was summed before.  A wave whose queries all see nothing yet
+// keeps m = -inf, weights 0.
+template <int NB>
+RV_DEV float softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, float sc, bool masked, float& m, float& l) {
+  float top = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < NB; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (masked) {
+        const int key = k0 + 16 * t + 4 * g + i;
+        if (!(key < kend && key <= last)) s[t][i] = -INFINITY;
+      }
+      top = fmaxf(top, s[t][i]);
+    }
+  top = rows4_max(top);
+  const float m_new = fmaxf(m, top * sc);
+  const float m_use = m_new == -INFINITY ? 0.f : m_new;
+  const float rescale = __builtin_amdgcn_exp2f(m - m_use);
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < NB; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], sc, -m_use));
+      sum += s[t][i];
+    }
+  l = l * rescale + rows4_sum(sum);
+  m = m_new;
+  return rescale;
+}
+
+// P of two 16-key blocks as hi and lo B operands.
+RV_DEV void split_p(const f32x4_t& s0, const f32x4_t& s1, bf16x8_t& hi, bf16x8_t& lo) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float p = j < 4 ? s0[j] : s1[j - 4];
+    const uint16_t h = f2bf(p);
+    hi[j] = __builtin_bit_cast(__bf16, h);
+    lo[j] = __builtin_bit_cast(__bf16, f2bf(p - bf2f(h)));
+  }
+}
+
+RV_DEV f32x4_t mfma(const u32x4& x, const bf16x8_t& y, const f32x4_t& acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), y, acc, 0, 0, 0);
+}
+
+// A masked key has weight 0, but 0 * inf is NaN: in tiles where some query does
+// not see every key, values that are not finite are taken out of the product and
+// the queries that see them get NaN instead (what the pair (inf, inf - inf)
+// stands for).  v: V operands of a 32-key chunk, vis: per key slot whether the
+// lane's query sees it.
+RV_DEV bool not_finite_bf16x2(uint32_t x) {
+  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
+template <int DT>
+RV_DEV bool any_not_finite(const u32x4 (&vh)[DT]) {
+  bool bad = false;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bad |= not_finite_bf16x2(vh[d][j]);
+  return __any(bad);
+}
+template <int DT>
+RV_DEV void take_out(u32x4 (&vh)[DT], u32x4 (&vl)[DT], int k0, int kend, int last, int g, f32x4_t (&O)[DT]) {
+  bf16x8_t vis;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int key = k0 + 4 * g + (j & 3) + 16 * (j >> 2);
+    vis[j] = (__bf16)(key < kend && key <= last ? 1.0f : 0.0f);
+  }
+#pragma unroll
+  for (int d = 0; d < DT; ++d) {
+    u32x4 mark;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t keep = 0, ones = 0;
+      if ((vh[d][j] & 0x7f80u) != 0x7f80u) keep |= 0xffffu;
+      else ones |= 0x3f80u;
+      if ((vh[d][j] & 0x7f800000u) != 0x7f800000u) keep |= 0xffff0000u;
+      else ones |= 0x3f800000u;
+      vh[d][j] &= keep;
+      vl[d][j] &= keep;
+      mark[j] = ones;
+    }
+    const f32x4_t seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, mark), vis,
+                                                                 f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (seen[i] > 0.f) O[d][i] = __builtin_nanf("");
+  }
+}
+
+// ----------------------------------------------------------- bf16, many queries
+// S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMAs, operands as pairs of planes
+// (three products each, lo lo dropped: 2^-16 of the result), 8 waves of one
+// 16-query tile.  The cache holds tiles in operand order (k_elem / v_elem): a
+// 64-key tile is four spans that go global -> LDS directly, double-buffered.
+template <int HD, int PART>
+__global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
+  constexpr int NW = 8, DC = HD / 32, DT = HD / 16, SPAN = kKB * HD;
+  constexpr int UPW = 4 * SPAN / 512 / NW;  // 1 KiB pieces each wave copies
+  __shared__ __attribute__((aligned(16))) uint16_t sm0[4][SPAN];
+  __shared__ __attribute__((aligned(16))) uint16_t sm1[4][SPAN];
+  Unit u;
+  if (!unit_of<PART>(a, blockIdx.x, u)) return;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  auto fetch = [&](uint16_t(&sm)[4][SPAN], int k0) {
+    const size_t at = tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + lane * 8;
+#pragma unroll
+    for (int i = 0; i < UPW; ++i) {
+      const int piece = w * UPW + i, sp = piece / (SPAN / 512), off = piece % (SPAN / 512) * 512;
+      const void* base = sp == 0 ? a.kc : sp == 1 ? a.kc2 : sp == 2 ? a.vc : a.vc2;
+      __builtin_amdgcn_global_load_lds((const void*)((const uint16_t*)base + at + off),
+                                       (__attribute__((address_space(3))) void*)(&sm[0][0] + sp * SPAN + off), 16, 0, 0);
+    }
+  };
+  fetch(sm0, u.kbeg);
+
+  const bool active = u.q_begin + 16 * w < u.nq;
+  const Query q = query_of<PART>(a, u, u.q_begin + 16 * w + (lane & 15));
+  const int first_last = first_limit<PART>(a, u);
+  u32x4 qh[DC], ql[DC];
+  load_query<HD>(a, q, g, qh, ql);
+  float m = -INFINITY, l = 0.f;
+  f32x4_t O[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto tile = [&](const uint16_t(&sm)[4][SPAN], int k0) {
+    if (!active) return;
+    f32x4_t s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+      const bf16x8_t h = __builtin_bit_cast(bf16x8_t, qh[c]), lo = __builtin_bit_cast(bf16x8_t, ql[c]);
+      u32x4 kh[4], kl[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        kh[t] = *(const u32x4*)(&sm[0][(t * DC + c) * 512 + lane * 8]);
+        kl[t] = *(const u32x4*)(&sm[1][(t * DC + c) * 512 + lane * 8]);
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t] = mfma(kh[t], h, s[t]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t] = mfma(kh[t], lo, s[t]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[t] = mfma(kl[t], h, s[t]);
+    }
+    const bool masked = k0 + kKB > u.kend || k0 + kKB - 1 > first_last;
+    const float rescale = softmax_step<4>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l);
+    if (__any(rescale != 1.0f)) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] *= rescale;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      bf16x8_t ph, pl;
+      split_p(s[2 * c], s[2 * c + 1], ph, pl);
+      u32x4 vh[DT], vl[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        vh[d] = *(const u32x4*)(&sm[2][(c * DT + d) * 512 + lane * 8]);
+        vl[d] = *(const u32x4*)(&sm[3][(c * DT + d) * 512 + lane * 8]);
+      }
+      if (masked && any_not_finite<DT>(vh)) take_out<DT>(vh, vl, k0 + 32 * c, u.kend, q.last, g, O);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] = mfma(vh[d], ph, O[d]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] = mfma(vh[d], pl, O[d]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] = mfma(vl[d], ph, O[d]);
+    }
+  };
+
+  // at the top of each half only the copy of the tile about to be used is in
+  // flight; after the barrier every wave has finished the one before, whose
+  // buffer takes the next
+  for (int k0 = u.kbeg; k0 < u.kend; k0 += 2 * kKB) {
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (k0 + kKB < u.kend) fetch(sm1, k0 + kKB);
+    tile(sm0, k0);
+    if (k0 + kKB >= u.kend) break;
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (k0 + 2 * kKB < u.kend) fetch(sm0, k0 + 2 * kKB);
+    tile(sm1, k0 + kKB);
+  }
+
+  // lane holds O^T[d = 16t + 4g + i][query lane%16]
+  if (!q.valid) return;
+  if (a.direct) {
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) put_out4<RV_BF16>(a, HD, q.row, q.head, 16 * d + 4 * g, O[d] * inv);
+    return;
+  }
+  const size_t e = part_index(a, u.slot, q.row, q.head);
+#pragma unroll
+  for (int d = 0; d < DT; ++d) *(f32x4_t*)(a.part_o + e * HD + 16 * d + 4 * g) = O[d];
+  if (g == 0) {
+    a.part_ml[2 * e] = m;
+    a.part_ml[2 * e + 1] = l;
+  }
+}
+
+// ----------------------------------------------------------- bf16, at most 16 queries
+// Decode steps: the 8 waves share the 16 queries and split the keys, wave w
+// taking tiles w, w + 8, ... of KT keys straight to registers; their states
+// merge in LDS.
+template <int HD, int PART>
+__global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
+  constexpr int KT = HD == 128 ? 32 : 64, NW = 8, NB = KT / 16, NC = KT / 32, DC = HD / 32, DT = HD / 16;
+  __shared__ __attribute__((aligned(16))) float red_o[NW][16][HD + 4];
+  __shared__ float red_m[NW][16], red_l[NW][16];
+  Unit u;
+  if (!unit_of<PART>(a, blockIdx.x, u)) return;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  u32x4 k[2][NB][DC], v[2][NC][DT];
+  // tiles past the last load that one again and are not used
+  const int last_tile = u.kbeg + (u.kend - 1 - u.kbeg) / KT * KT;
+  auto at = [&](int k0) { return tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + (size_t)(k0 % kKB) * HD + lane * 8; };
+  auto load_k = [&](size_t o) {
+#pragma unroll
+    for (int pl = 0; pl < 2; ++pl)
+#pragma unroll
+      for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+          k[pl][t][c] = *(const u32x4*)((const uint16_t*)(pl ? a.kc2 : a.kc) + o + (t * DC + c) * 512);
+  };
+  auto load_v = [&](size_t o) {
+#pragma unroll
+    for (int pl = 0; pl < 2; ++pl)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          v[pl][c][d] = *(const u32x4*)((const uint16_t*)(pl ? a.vc2 : a.vc) + o + (c * DT + d) * 512);
+  };
+  int k0 = u.kbeg + w * KT;
+  size_t next = at(min(k0, last_tile));
+  if (k0 < u.kend) {
+    load_k(next);
+    load_v(next);
+  }
+  next = at(min(k0 + NW * KT, last_tile));
+  const Query q = query_of<PART>(a, u, u.q_begin + (lane & 15));
+  const int first_last = first_limit<PART>(a, u);
+  u32x4 qh[DC], ql[DC];
+  load_query<HD>(a, q, g, qh, ql);
+  float m = -INFINITY, l = 0.f;
+  f32x4_t O[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  for (; k0 < u.kend; k0 += NW * KT) {
+    f32x4_t s[NB];
+#pragma unroll
+    for (int t = 0; t < NB; ++t) s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+      const bf16x8_t h = __builtin_bit_cast(bf16x8_t, qh[c]), lo = __builtin_bit_cast(bf16x8_t, ql[c]);
+#pragma unroll
+      for (int t = 0; t < NB; ++t) s[t] = mfma(k[0][t][c], h, s[t]);
+#pragma unroll
+      for (int t = 0; t < NB; ++t) s[t] = mfma(k[0][t][c], lo, s[t]);
+#pragma unroll
+      for (int t = 0; t < NB; ++t) s[t] = mfma(k[1][t][c], h, s[t]);
+    }
+    load_k(next);
+    const bool masked = k0 + KT > u.kend || k0 + KT - 1 > first_last;
+    const float rescale = softmax_step<NB>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) O[d] *= rescale;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      bf16x8_t ph, pl;
+      split_p(s[2 * c], s[2 * c + 1], ph, pl);
+      if (masked && any_not_finite<DT>(v[0][c])) take_out<DT>(v[0][c], v[1][c], k0 + 32 * c, u.kend, q.last, g, O);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] = mfma(v[0][c][d], ph, O[d]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] = mfma(v[0][c][d], pl, O[d]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] = mfma(v[1][c][d], ph, O[d]);
+    }
+    load_v(next);
+    next = at(min(k0 + 2 * NW * KT, last_tile));
+  }
+
+  // merge the waves: one without tiles has m = -inf, l = 0, O = 0
+#pragma unroll
+  for (int d = 0; d < DT; ++d) *(f32x4_t*)&red_o[w][lane & 15][16 * d + 4 * g] = O[d];
+  if (g == 0) {
+    red_m[w][lane & 15] = m;
+    red_l[w][lane & 15] = l;
+  }
+  __syncthreads();
+  const int oq = tid / (HD / 4), od = tid % (HD / 4) * 4;
+  if (oq >= 16) return;
+  const Query oqr = query_of<PART>(a, u, u.q_begin + oq);
+  if (!oqr.valid) return;
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) M = fmaxf(M, red_m[i][oq]);
+  f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    const float f = red_m[i][oq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[i][oq] - M);
+    L += red_l[i][oq] * f;
+    x += *(const f32x4_t*)&red_o[i][oq][od] * f;
+  }
+  if (a.direct) {
+    put_out4<RV_BF16>(a, HD, oqr.row, oqr.head, od, x * (1.0f / L));
+    return;
+  }
+  const size_t e = part_index(a, u.slot, oqr.row, oqr.head);
+  *(f32x4_t*)(a.part_o + e * HD + od) = x;
+  if (od == 0) {
+    a.part_ml[2 * e] = M;
+    a.part_ml[2 * e + 1] = L;
+  }
+}
+
+// As take_out, for four keys of an fp32 cache, where infinities keep their sign.
+template <int DC>
+RV_DEV void take_out_f32(float (&v)[DC], bool vis, f32x4_t (&o)[DC]) {
+  const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+  const float see = vis ? 1.f : 0.f;
+#pragma unroll
+  for (int e = 0; e < DC; ++e) {
+    const f32x4_t nan = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e] != v[e] ? 1.f : 0.f, see, zero, 0, 0, 0);
+    const f32x4_t up = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e] == INFINITY ? 1.f : 0.f, see, zero, 0, 0, 0);
+    const f32x4_t down = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e] == -INFINITY ? 1.f : 0.f, see, zero, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (up[i] > 0.f) o[e][i] += INFINITY;
+      if (down[i] > 0.f) o[e][i] -= INFINITY;
+      if (nan[i] > 0.f) o[e][i] = __builtin_nanf("");
+    }
+    if (!__builtin_isfinite(v[e])) v[e] = 0.f;
+  }
+}
+
+// ----------------------------------------------------------- fp32
+// One wave per (16 queries, run, kv head) on 16x16x4 fp32 MFMAs; K and V come
+// straight from the row-major cache.  The k slots of an MFMA may hold any four
+// dims that both operands agree on, so a lane's 16-byte load of dims
+// 16c + 4(l/16) .. +3 feeds four MFMAs, and P comes straight from the scores.
+template <int HD, int PART>
+__global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
+  constexpr int DC = HD / 16;
+  Unit u;
+  if (!unit_of<PART>(a, blockIdx.x, u)) return;
+  const int lane = threadIdx.x, g = lane >> 4, c16 = lane & 15;
+  const Query q = query_of<PART>(a, u, u.q_begin + c16);
+  f32x4_t qv[DC];
+#pragma unroll
+  for (int c = 0; c < DC; ++c) {
+    const int d = q.head * HD + 16 * c + 4 * g;
+    if (a.q_kind == ROWS_OPERAND) {
+      qv[c] = *(const f32x4_t*)((const char*)a.q + operand_offset(q.row, d, a.n_heads * HD, 4));
+    } else if (a.q_kind == RV_F32) {
+      qv[c] = *(const f32x4_t*)((const float*)a.q + (size_t)q.row * a.ldq + d);
+    } else {
+      uint16_t h[4];
+      memcpy(h, (const uint16_t*)a.q + (size_t)q.row * a.ldq + d, 8);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) qv[c][j] = bf2f(h[j]);
+    }
+  }
+  f32x4_t o[DC];
+#pragma unroll
+  for (int t = 0; t < DC; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  const int first_last = first_limit<PART>(a, u);
+
+  for (int k0 = u.kbeg; k0 < u.kend; k0 += kKB) {
+    const size_t base = tile_base<HD>(a, u.seq, u.kvh, k0 / kKB);
+    const float* kb = (const float*)a.kc + base;
+    const float* vb = (const float*)a.vc + base;
+    f32x4_t s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const float* kr = kb + (16 * t + c16) * HD + 4 * g;
+      f32x4_t kv[DC];
+#pragma unroll
+      for (int c = 0; c < DC; ++c) kv[c] = *(const f32x4_t*)(kr + 16 * c);
+#pragma unroll
+      for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[c][i], qv[c][i], s[t], 0, 0, 0);
+    }
+    const bool masked = k0 + kKB > u.kend || k0 + kKB - 1 > first_last;
+    const float rescale = softmax_step<4>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l);
+#pragma unroll
+    for (int t = 0; t < DC; ++t) o[t] *= rescale;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int kk = 16 * t + 4 * g + i;
+        const float* vr = vb + kk * HD + c16 * DC;
+        float v[DC];
+        if constexpr (DC == 2) {
+          const float2 x = *(const float2*)vr;
+          v[0] = x.x;
+          v[1] = x.y;
+        } else {
+#pragma unroll
+          for (int e = 0; e < DC; e += 4) {
+            const f32x4_t x = *(const f32x4_t*)(vr + e);
+#pragma unroll
+            for (int f = 0; f < 4; ++f) v[e + f] = x[f];
+          }
+        }
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < DC; ++e) bad |= !__builtin_isfinite(v[e]);
+        if (masked && __any(bad)) take_out_f32<DC>(v, k0 + kk < u.kend && k0 + kk <= q.last, o);
+#pragma unroll
+        for (int e = 0; e < DC; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], s[t][i], o[e], 0, 0, 0);
+      }
+  }
+  if (!q.valid) return;
+  // lane holds dims (4g + i) DC + t of its query: a run of 4 DC
+  const size_t e = part_index(a, u.slot, q.row, q.head);
+  const float inv = a.direct ? 1.0f / l : 1.0f;
+#pragma unroll
+  for (int y = 0; y < DC; ++y) {
+    f32x4_t x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = o[(4 * y + j) % DC][(4 * y + j) / DC] * inv;
+    if (a.direct) put_out4<RV_F32>(a, HD, q.row, q.head, 4 * g * DC + 4 * y, x);
+    else *(f32x4_t*)(a.part_o + e * HD + 4 * g * DC + 4 * y) = x;
+  }
+  if (!a.direct && g == 0) {
+    a.part_ml[2 * e] = m;
+    a.part_ml[2 * e + 1] = l;
+  }
+}
+
+// ----------------------------------------------------------- merge
+// hd / 4 lanes per (row, head): one pass over the runs that had keys for the
+// row, shared runs first, in batches whose loads are issued together.
+template <int DT, int HD>
+__global__ __launch_bounds__(256) void k_share_merge(ShareArgs a) {
+  constexpr int LPQ = HD / 4, BATCH = 8;
+  const int b = blockIdx.y, n = a.row0[b + 1] - a.row0[b];
+  const int i = blockIdx.x * (256 / LPQ) + threadIdx.x / LPQ, d = threadIdx.x % LPQ * 4;
+  if (i >= n * a.n_heads) return;
+  const int r = i / a.n_heads, head = i % a.n_heads, row = a.row0[b] + r;
+  const int g = a.p.group_of[b], k0 = g == 255 ? 0 : a.p.tiles[g] * kKB;
+  const int n_sh = g == 255 ? 0 : (k0 + a.p.sh.ks - 1) / a.p.sh.ks;
+  const int n_own = (a.pos0[b] + r - k0) / a.p.own.ks + 1;
+  const int skip = (a.p.groups ? a.p.sh.ns : 0) - n_sh;  // slots of shared runs that this row has not
+  const size_t e0 = part_index(a, 0, row, head), stride = (size_t)a.p.rows * a.n_heads;
+  float M = -INFINITY, L = 0.f;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < n_sh + n_own; s0 += BATCH) {
+    float m[BATCH], l[BATCH];
+    f32x4_t x[BATCH];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int s = min(s0 + u, n_sh + n_own - 1);  // past the last: that one again, weight 0
+      const size_t e = e0 + (size_t)(s < n_sh ? s : s + skip) * stride;
+      m[u] = a.part_ml[2 * e];
+      l[u] = a.part_ml[2 * e + 1];
+      x[u] = *(const f32x4_t*)(a.part_o + e * HD + d);
+    }
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) top = fmaxf(top, m[u]);
+    const float base = top == -INFINITY ? 0.f : top, keep = __builtin_amdgcn_exp2f(M - base);
+    L *= keep;
+    acc *= keep;
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const float f = s0 + u < n_sh + n_own ? __builtin_amdgcn_exp2f(m[u] - base) : 0.f;
+      L += l[u] * f;
+      acc += x[u] * f;
+    }
+    M = top;
+  }
+  put_out4<DT>(a, HD, row, head, d, acc * (1.0f / L));
+}
+
+template <int HD, int PART>
+hipError_t launch_part(int dtype, const ShareArgs& a, hipStream_t st) {
+  const SharePart& sp = PART ? a.p.own : a.p.sh;
+  const size_t units = (size_t)sp.ns * a.n_kv * (PART ? a.p.nseq : a.p.groups);
+  const size_t grid = (units + 7) / 8 * 8 * sp.nqg;
+  if (!grid) return hipSuccess;
+  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  if (dtype == RV_F32) k_share_f32<HD, PART><<<(unsigned)grid, 64, 0, st>>>(a);
+  else if (sp.qpw == 16) k_share_few<HD, PART><<<(unsigned)grid, 512, 0, st>>>(a);
+  else k_share_many<HD, PART><<<(unsigned)grid, 512, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <int HD>
+hipError_t launch_all(int dtype, ShareArgs& a, hipStream_t st) {
+  a.direct = a.p.groups == 0 && a.p.own.ns == 1;
+  if (a.p.groups)
+    if (hipError_t e = launch_part<HD, 0>(dtype, a, st); e != hipSuccess) return e;
+  if (hipError_t e = launch_part<HD, 1>(dtype, a, st); e != hipSuccess) return e;
+  if (a.direct) return hipSuccess;
+  int longest = 0;
+  for (int b = 0; b < a.p.nseq; ++b) longest = std::max(longest, a.row0[b + 1] - a.row0[b]);
+  constexpr int per = 256 / (HD / 4);
+  const dim3 grid((unsigned)(((size_t)longest * a.n_heads + per - 1) / per), a.p.nseq);
+  if (dtype == RV_BF16) k_share_merge<RV_BF16, HD><<<grid, 256, 0, st>>>(a);
+  else k_share_merge<RV_F32, HD><<<grid, 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_share(int dtype, int hd, ShareArgs& a, hipStream_t st) {
+  switch (hd) {
+    case 32: return launch_all<32>(dtype, a, st);
+    case 64: return launch_all<64>(dtype, a, st);
+    case 128: return launch_all<128>(dtype, a, st);
+  }
+  return hipErrorInvalidValue;
+}

@@ -4,10 +4,12 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <memory>
+#include <new>
 #include <string>
 #include <vector>
 
-#include "rv_internal.h"
+#include "rv_state.h"
 
 namespace {
 
@@ -27,16 +29,6 @@ rv_status rv_fail(rv_status s, const char* fmt, ...) {
 
 namespace {
 
-
-rv_status hip_fail(hipError_t e, const char* what) {
-  return rv_fail(RV_E_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-#define HIP_TRY(expr, what)                 \
-  do {                                      \
-    hipError_t e_ = (expr);                 \
-    if (e_ != hipSuccess) return hip_fail(e_, what); \
-  } while (0)
 
 constexpr size_t kAlign = 256;
 constexpr int kVocabChunk = 2048;    // vocabulary chunk of the LM-head tail (8 entries per thread)
@@ -64,62 +56,6 @@ uint64_t splitmix_finalise(uint64_t z) {
 }
 
 }  // namespace
-
-struct rv_model {
-  rv_config cfg;
-  uint64_t seed;
-  char* base;
-  size_t bytes;
-  int es;
-  MatDesc qkv, o, gateup, down, lm;
-  void* embed;
-  float* norm_f;
-  void* lm_head;
-  std::vector<void*> w_qkv, w_o, w_gateup, w_down;
-  std::vector<float*> n1, n2;
-};
-
-struct rv_cache {
-  rv_model* m;
-  int B, max_len, max_block, max_drafts;
-  int kv_len;  // cached positions per (sequence, kv head): max_len rounded up to whole 64-key tiles
-  char* base;
-  size_t bytes;
-  int rows_cap, out_rows_cap, r1_cap, nchunk;
-  size_t kv_layer_elems;
-  char* kc;   // K cache [layer][b][kv_head][kv_len x hd] (order: put_k4 / put_v4): bf16 hi plane, or fp32
-  char* vc;
-  char* kc2;  // bf16 lo planes (bf16 models)
-  char* vc2;
-  int* ids;
-  float* rope_cos;
-  float* rope_sin;
-  int* seq_bad;
-  int *row_pos, *row_seq, *row_bad;
-  int *seg_b, *seg_row0, *seg_n, *seg_pos0;
-  float* h;
-  // matmul operands: first plane (bf16 hi, or fp32) and bf16 lo plane
-  void *xn, *xn2, *qbuf, *qbuf2, *att, *att2, *act, *act2, *lm_x, *lm_x2;
-  size_t part_entries;
-  float *part_o, *part_ml;
-  float* gpart;  // k-group partials of a split matmul [gk][rows][max(d_model, qkv rows)], gk*rows <= gpart_rows
-  int gpart_rows;
-  float *logits, *z, *lp, *hpart, *lse, *margins, *entropy;
-  int* lm_src;                      // block row of each LM-head row of the last verify
-  int last_R1;                      // fused rows of the last verify
-  uint8_t last_kb[RV_MAX_BATCH];    // its per-sequence draft counts
-  int* argmax;
-  int last_k = -1;
-  int force_rows = 0, force_mt = 0, force_gk = 0;  // rv_debug_force_matmul
-  // event profiler
-  bool prof = false;
-  std::vector<hipEvent_t> prof_ev;   // pairs: start, stop
-  std::vector<int> prof_cls;
-  size_t prof_used = 0;
-  ~rv_cache() {
-    for (hipEvent_t e : prof_ev) (void)hipEventDestroy(e);
-  }
-};
 
 namespace {
 
@@ -235,6 +171,7 @@ size_t cache_layout(rv_cache* c, void* buf) {
   c->entropy = cv.take<float*>((size_t)2 * c->r1_cap * 4);
   c->lm_src = cv.take<int*>((size_t)c->out_rows_cap * 4);
   c->argmax = cv.take<int*>((size_t)c->r1_cap * 4);
+  c->tile_own = cv.take<int*>((size_t)c->B * (c->kv_len / kTile) * 4);
   return align_up(cv.off, kAlign);
 }
 
@@ -330,8 +267,9 @@ hipError_t run_gemm(const rv_cache* c, int epi, GemmArgs g, const MatPlan& p, hi
 // qmax: queries per (segment, kv head); kmax: 1 + largest position in the plan.
 // With split_last the last down projection may leave k-group partials in
 // c->gpart; *pending_out then gives their count (the final norm adds them).
+// share: attention over shared tiles, planned (NULL: no sequence shares any).
 rv_status run_layers(rv_cache* c, int M, int nseg, int max_seg_rows, int kmax, const int* h_seg_end,
-                     const int* h_seg_rows, bool split_last, int* pending_out, hipStream_t st) {
+                     const int* h_seg_rows, bool split_last, int* pending_out, ShareArgs* share, hipStream_t st) {
   rv_model* m = c->m;
   const rv_config& mc = m->cfg;
   const int dt = mc.dtype, d = mc.d_model, hd = mc.head_dim;
@@ -414,13 +352,36 @@ rv_status run_layers(rv_cache* c, int M, int nseg, int max_seg_rows, int kmax, c
       // agent-scope release per workgroup, an L2 writeback each: measured
       // slower than the extra launch.)
       Prof pf(c, RV_PROF_QKV, st);
+      QkvFinish qf{c->gpart, p_qkv.gk(), M, g.N, g.q_rows, g.k_rows, hd, mc.n_heads, mc.n_kv_heads, c->kv_len,
+                   c->row_pos, c->row_seq, c->rope_cos, c->rope_sin, c->qbuf, c->qbuf2, kc, vc, kc2, vc2};
+      if (m->q_gain) {
+        qf.q_gain = m->q_gain + (size_t)l * hd;
+        qf.k_gain = m->k_gain + (size_t)l * hd;
+        qf.eps = mc.rms_eps;
+      }
       if (p_qkv.gk() > 1) {
         g.P = c->gpart;
         g.ldy = g.N;
         HIP_TRY(run_gemm(c, EPI_RESID, g, p_qkv, st), "qkv");
-        QkvFinish qf{c->gpart, p_qkv.gk(), M, g.N, g.q_rows, g.k_rows, hd, mc.n_heads, mc.n_kv_heads, c->kv_len,
-                     c->row_pos, c->row_seq, c->rope_cos, c->rope_sin, c->qbuf, c->qbuf2, kc, vc, kc2, vc2};
         HIP_TRY(launch_qkv_finish(dt, qf, st), "qkv finish");
+      } else if (m->q_gain) {
+        // a norm needs whole heads, which the matrix kernels' epilogue has not:
+        // the product goes through the partial buffer, as many rows at a time as
+        // that holds (a multiple of 64), and the finish kernel completes them
+        for (int r0 = 0; r0 < M; r0 += c->gpart_rows) {
+          GemmArgs gc = g;
+          const size_t off = operand_offset(r0, 0, d, m->es);
+          gc.X = (const char*)g.X + off;
+          gc.X2 = g.X2 ? (const char*)g.X2 + off : nullptr;
+          gc.M = std::min(c->gpart_rows, M - r0);
+          gc.Y = c->gpart;
+          gc.ldy = g.N;
+          HIP_TRY(run_gemm(c, EPI_STORE, gc, plan_for(c, EPI_STORE, gc.M, gc.N, gc.K, false), st), "qkv");
+          qf.gk = 1;
+          qf.M = gc.M;
+          qf.tok0 = r0;
+          HIP_TRY(launch_qkv_finish(dt, qf, st), "qkv finish");
+        }
       } else {
         HIP_TRY(run_gemm(c, EPI_QKV, g, p_qkv, st), "qkv");
       }
@@ -430,11 +391,18 @@ rv_status run_layers(rv_cache* c, int M, int nseg, int max_seg_rows, int kmax, c
     at.vc = vc;
     at.kc2 = kc2;
     at.vc2 = vc2;
-    {
+    if (share) {
+      share->kc = kc;
+      share->vc = vc;
+      share->kc2 = kc2;
+      share->vc2 = vc2;
+      Prof pf(c, RV_PROF_ATTN, st);
+      HIP_TRY(launch_share(dt, hd, *share, st), "attention");
+    } else {
       Prof pf(c, RV_PROF_ATTN, st);
       HIP_TRY(launch_attention(dt, at, ap.n_qgroups, ap.qpw, st), "attention");
     }
-    if (ap.nsplit > 1) {  // one split: the output is final
+    if (!share && ap.nsplit > 1) {  // one split: the output is final
       Prof pf(c, RV_PROF_COMBINE, st);
       HIP_TRY(launch_attn_combine(dt, at, st), "attention combine");
     }
@@ -622,7 +590,19 @@ rv_status rv_cache_create(rv_model* m, int32_t batch, int32_t max_len, int32_t m
   if (s != RV_OK) return s;
   if (!d_buf || !out) return rv_fail(RV_E_ARG, "d_buf and out must not be NULL");
   if (buf_bytes < need) return rv_fail(RV_E_BUFFER, "cache buffer has %zu bytes, needs %zu", buf_bytes, need);
-  rv_cache* c = new rv_cache();
+  std::unique_ptr<rv_cache> c;
+  std::vector<float> cs, sn;
+  std::vector<int> own;
+  const int hh = m->cfg.head_dim / 2;
+  try {
+    c.reset(new rv_cache());
+    cs.resize((size_t)max_len * hh);
+    sn.resize((size_t)max_len * hh);
+    c->tiles.create(batch, (max_len + kTile - 1) / kTile);
+    own.assign(c->tiles.own.begin(), c->tiles.own.end());
+  } catch (const std::bad_alloc&) {
+    return rv_fail(RV_E_STATE, "out of host memory");
+  }
   c->m = m;
   c->B = batch;
   c->max_len = max_len;
@@ -630,25 +610,22 @@ rv_status rv_cache_create(rv_model* m, int32_t batch, int32_t max_len, int32_t m
   c->max_drafts = max_drafts;
   c->base = (char*)d_buf;
   c->bytes = need;
-  cache_layout(c, d_buf);
+  cache_layout(c.get(), d_buf);
   // rotary table: angle p * base^(-2i/hd) in fp64, stored as fp32
-  const int hh = m->cfg.head_dim / 2;
-  std::vector<float> cs((size_t)max_len * hh), sn((size_t)max_len * hh);
+  double theta[64];
+  for (int i = 0; i < hh; ++i) theta[i] = std::pow((double)m->cfg.rope_base, -2.0 * i / m->cfg.head_dim);
   for (int p = 0; p < max_len; ++p)
     for (int i = 0; i < hh; ++i) {
-      const double theta = std::pow((double)m->cfg.rope_base, -2.0 * i / m->cfg.head_dim);
-      const double ang = (double)p * theta;
+      const double ang = (double)p * theta[i];
       cs[(size_t)p * hh + i] = (float)std::cos(ang);
       sn[(size_t)p * hh + i] = (float)std::sin(ang);
     }
   hipError_t e = hipMemset(d_buf, 0, need);
   if (e == hipSuccess) e = hipMemcpy(c->rope_cos, cs.data(), cs.size() * 4, hipMemcpyHostToDevice);
   if (e == hipSuccess) e = hipMemcpy(c->rope_sin, sn.data(), sn.size() * 4, hipMemcpyHostToDevice);
-  if (e != hipSuccess) {
-    delete c;
-    return hip_fail(e, "cache setup");
-  }
-  *out = c;
+  if (e == hipSuccess) e = hipMemcpy(c->tile_own, own.data(), own.size() * 4, hipMemcpyHostToDevice);
+  if (e != hipSuccess) return hip_fail(e, "cache setup");
+  *out = c.release();
   return RV_OK;
 }
 
@@ -674,6 +651,7 @@ rv_status rv_prefill_cache(rv_cache* c, const int32_t* d_prefix_ids, int32_t ld,
   si.ids = c->ids;
   si.seq_bad = c->seq_bad;
   for (int b = 0; b < c->B; ++b) si.L[b] = h_prefix_len[b];
+  if (rv_status s = reset_owners(c, st); s != RV_OK) return s;
   HIP_TRY(launch_store_ids(si, st), "store ids");
 
   // Chunks of up to rows_cap rows over all (sequence, position < L-1).
@@ -705,7 +683,7 @@ rv_status rv_prefill_cache(rv_cache* c, const int32_t* d_prefix_ids, int32_t ld,
     }
     int seg_end[RV_MAX_SEGS];
     for (int i = 0; i < ch.nseg; ++i) seg_end[i] = ch.spos0[i] + ch.sn[i];
-    rv_status s = run_layers(c, ch.rows, ch.nseg, ch.max_n, ch.kmax, seg_end, ch.sn, false, nullptr, st);
+    rv_status s = run_layers(c, ch.rows, ch.nseg, ch.max_n, ch.kmax, seg_end, ch.sn, false, nullptr, nullptr, st);
     if (s != RV_OK) return s;
   }
   c->last_k = -1;
@@ -813,6 +791,7 @@ rv_status verify_impl(rv_cache* c, const int32_t* h_prefix_len, const int32_t* d
     if ((long long)L - 1 + S > c->max_len || (long long)L + kk + 1 > c->max_len)
       return rv_fail(RV_E_CAPACITY, "sequence %d: block of %lld rows at length %d exceeds max_len=%d", b, S, L,
                   c->max_len);
+    if (rv_status ws = check_writable(c, b, L - 1, (int)S); ws != RV_OK) return ws;
     kmax = std::max(kmax, (int)(L - 1 + S));
     seg_end[b] = (int)(L - 1 + S);
     seg_rows[b] = (int)S;
@@ -855,8 +834,27 @@ rv_status verify_impl(rv_cache* c, const int32_t* h_prefix_len, const int32_t* d
     HIP_TRY(launch_plan_verify(dt, pv, st), "verify plan");
   }
 
+  // block rows over tiles that sequences share (rv_cache_fork): the rows of
+  // sequence b follow those of b - 1, at positions L_b - 1 ..
+  ShareArgs share{};
+  if (c->tiles.foreign) {
+    int pos0[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1];
+    row0[0] = 0;
+    for (int b = 0; b < c->B; ++b) {
+      pos0[b] = h_prefix_len[b] - 1;
+      row0[b + 1] = row0[b] + seg_rows[b];
+    }
+    plan_attend(c, pos0, row0, share);
+    share.q = c->qbuf;
+    share.q2 = c->qbuf2;
+    share.out = c->att;
+    share.out2 = c->att2;
+    share.q_kind = share.o_kind = ROWS_OPERAND;
+  }
+
   int pending = 0;
-  rv_status s = run_layers(c, M, c->B, S_max, kmax, seg_end, seg_rows, true, &pending, st);
+  rv_status s = run_layers(c, M, c->B, S_max, kmax, seg_end, seg_rows, true, &pending,
+                           c->tiles.foreign ? &share : nullptr, st);
   if (s != RV_OK) return s;
 
   // LM head on the 2(k_b+1) rows per sequence that Algorithm 1 reads.
@@ -997,22 +995,33 @@ rv_status rv_debug_export_kv(const rv_cache* c, int32_t layer, int32_t seq, int3
   const int planes = es == 2 ? 2 : 1;
   const size_t plane = row * mc.n_kv_heads;
   if (dst_bytes < plane * planes) return rv_fail(RV_E_BUFFER, "destination needs %zu bytes", plane * planes);
-  const size_t blk = (size_t)layer * c->kv_layer_elems + (size_t)seq * mc.n_kv_heads * c->kv_len * hd;
   hipStream_t st = (hipStream_t)stream;
-  if (es == 2) {
-    // bf16 caches are stored in attention operand order: copy out row-major
-    HIP_TRY(launch_export_kv((uint16_t*)c->kc + blk, (uint16_t*)c->kc2 + blk, (int)hd, mc.n_kv_heads, c->kv_len, pos0,
-                             npos, false, d_k, st),
-            "export");
-    HIP_TRY(launch_export_kv((uint16_t*)c->vc + blk, (uint16_t*)c->vc2 + blk, (int)hd, mc.n_kv_heads, c->kv_len, pos0,
-                             npos, true, d_v, st),
-            "export");
-    return RV_OK;
+  // one span for each slot that the sequence's tiles lie in (its own, unless forked)
+  for (int p = pos0; p < pos0 + npos;) {
+    const int slot = c->tiles.at(seq, p / kTile);
+    int t = p / kTile + 1;
+    while (t * kTile < pos0 + npos && c->tiles.at(seq, t) == slot) ++t;
+    const int n = std::min(t * kTile, pos0 + npos) - p, done = p - pos0;
+    const size_t blk = (size_t)layer * c->kv_layer_elems + (size_t)slot * mc.n_kv_heads * c->kv_len * hd;
+    if (es == 2) {
+      // bf16 caches are stored in attention operand order: copy out row-major
+      HIP_TRY(launch_export_kv((uint16_t*)c->kc + blk, (uint16_t*)c->kc2 + blk, (int)hd, mc.n_kv_heads, c->kv_len, p, n,
+                               false, d_k, npos, done, st),
+              "export");
+      HIP_TRY(launch_export_kv((uint16_t*)c->vc + blk, (uint16_t*)c->vc2 + blk, (int)hd, mc.n_kv_heads, c->kv_len, p, n,
+                               true, d_v, npos, done, st),
+              "export");
+    } else {
+      const size_t off = (blk + (size_t)p * hd) * es, spitch = (size_t)c->kv_len * hd * es, at = done * hd * es;
+      HIP_TRY(hipMemcpy2DAsync((char*)d_k + at, row, c->kc + off, spitch, n * hd * es, mc.n_kv_heads,
+                               hipMemcpyDeviceToDevice, st),
+              "copy");
+      HIP_TRY(hipMemcpy2DAsync((char*)d_v + at, row, c->vc + off, spitch, n * hd * es, mc.n_kv_heads,
+                               hipMemcpyDeviceToDevice, st),
+              "copy");
+    }
+    p += n;
   }
-  const size_t off = (blk + (size_t)pos0 * hd) * es;
-  const size_t spitch = (size_t)c->kv_len * hd * es;
-  HIP_TRY(hipMemcpy2DAsync(d_k, row, c->kc + off, spitch, row, mc.n_kv_heads, hipMemcpyDeviceToDevice, st), "copy");
-  HIP_TRY(hipMemcpy2DAsync(d_v, row, c->vc + off, spitch, row, mc.n_kv_heads, hipMemcpyDeviceToDevice, st), "copy");
   return RV_OK;
 }
 

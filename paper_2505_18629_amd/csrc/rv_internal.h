@@ -3,6 +3,7 @@
 #pragma once
 #include "rv_common.h"
 #include "rv_plan.h"
+#include "rv_tiles.h"
 
 // ---------------------------------------------------------------- init
 hipError_t launch_init_packed(int dtype, void* dst, const MatDesc& md, uint64_t t0, uint64_t t1, uint64_t t2,
@@ -106,9 +107,9 @@ hipError_t launch_attention(int dtype, const AttnArgs& a, int n_qgroups, int qpw
 hipError_t launch_attn_combine(int dtype, const AttnArgs& a, hipStream_t st);
 // Copies positions pos0 .. pos0+npos-1 of every kv head of one sequence out of
 // a bf16 K (is_v false) or V cache block into row-major planes
-// dst[2][n_kv][npos][hd] (hi, lo).  src: the sequence's first (kv head) block.
+// dst[2][n_kv][dst_npos][hd] (hi, lo) from position `done` on.  src: the slot's first (kv head) block.
 hipError_t launch_export_kv(const void* src_hi, const void* src_lo, int hd, int n_kv, int kv_len, int pos0,
-                            int npos, bool is_v, void* dst, hipStream_t st);
+                            int npos, bool is_v, void* dst, int dst_npos, int done, hipStream_t st);
 
 // ---------------------------------------------------------------- norms and planning
 // RMSNorm of rows of the fp32 residual h into matmul operands (out, out2).  Output row r
@@ -151,6 +152,9 @@ struct QkvFinish {
   void* vc;
   void* kc2;
   void* vc2;
+  int tok0 = 0;            // token of the partials' first row
+  const float *q_gain = nullptr, *k_gain = nullptr;  // [hd] norms of queries and keys (rv_model_qk_norm)
+  float eps = 0.f;
 };
 hipError_t launch_qkv_finish(int dtype, const QkvFinish& a, hipStream_t st);
 
@@ -235,6 +239,76 @@ struct HeadArgs {
 hipError_t launch_head(const HeadArgs& a, hipStream_t st);
 // dst[i] = exp(src[i]) for i < n.
 hipError_t launch_exp(const float* src, float* dst, size_t n, hipStream_t st);
+
+// ---------------------------------------------------------------- operators on the cache
+// Rows of sequence b: row0[b] .. row0[b+1]-1 at positions pos[b] ..; blk0 counts
+// the 32-position blocks they touch (span_blocks).
+struct AppendArgs {
+  const void *q, *k, *v;     // rows of heads x hd values, row strides ldq, ldk, ldv (elements)
+  void* q_out;
+  size_t ldq, ldk, ldv, ldqo;
+  const float *q_gain, *k_gain;  // [hd], or NULL: not normalised
+  float eps;
+  bool rotate;
+  const float *rope_cos, *rope_sin;
+  void *kc, *vc, *kc2, *vc2;  // this layer's cache planes
+  int n_heads, n_kv, kv_len, B, hpw;  // n_heads 0: no q; hpw is the launcher's
+  int pos[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1], blk0[RV_MAX_BATCH + 1];
+};
+struct ReadArgs {
+  void *k, *v;
+  size_t ldk, ldv;
+  const void *kc, *vc, *kc2, *vc2;
+  const int* own;  // [B][kv_len / 64]: slot of each tile
+  int n_kv, kv_len, B, hpw;
+  int pos[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1], blk0[RV_MAX_BATCH + 1];
+};
+static_assert(sizeof(AppendArgs) <= 4096 && sizeof(ReadArgs) <= 4096, "kernel arguments");
+int span_blocks(int pos, int rows);
+// io: element type of the rows.  blk0[B] > 0.
+hipError_t launch_append(int dtype, int io, int hd, int max_rows, AppendArgs& a, hipStream_t st);
+hipError_t launch_read(int dtype, int io, int hd, int max_rows, ReadArgs& a, hipStream_t st);
+
+// Moves p over tiles [tile0, tile1) of every plane, layer and kv head.
+struct CopyArgs {
+  void* plane[4];
+  int planes, layers, n_kv, max_len, tile0, tile1;
+  size_t layer_vecs, slot_vecs, head_vecs;  // strides in 16-byte values
+  int tile_vecs;
+  int* ids;
+  int* seq_bad;
+  CopyProgram p;
+};
+static_assert(sizeof(CopyArgs) <= 4096, "kernel arguments");
+hipError_t launch_copy(const CopyArgs& a, bool with_ids, hipStream_t st);
+
+struct OwnArgs {
+  int* own;
+  int T, src, whole;
+  uint8_t seq[RV_MAX_BATCH];
+};
+hipError_t launch_own(const OwnArgs& a, int n, hipStream_t st);
+
+// Attention over a cache whose sequences may share tiles (rv_tiles.h: SharePlan).
+enum { ROWS_OPERAND = 2 };  // q / out as operand planes; else rows of RV_F32 or RV_BF16
+struct ShareArgs {
+  const void *q, *q2;    // rows [rows][ldq], or operand planes
+  void *out, *out2;
+  size_t ldq, ldo;
+  const void *kc, *vc, *kc2, *vc2;
+  const int* own;        // [B][T], or NULL where every tile is the sequence's own
+  float *part_o, *part_ml;  // [slot][row][head][hd] and [2]: (maximum in log2 units, sum)
+  int q_kind, o_kind;
+  int n_heads, n_kv, kv_len;
+  float scale_log2;
+  int part;              // 0: shared keys, 1: the sequences' own keys (the launcher's)
+  int direct;            // one run and no groups: the output is final
+  int pos0[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1];
+  SharePlan p;
+};
+static_assert(sizeof(ShareArgs) <= 4096, "kernel arguments");
+// Every launch of one call: shared part, own part, merge.
+hipError_t launch_share(int dtype, int hd, ShareArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- host helpers
 // Records the calling thread's error message (rv_last_error) and returns s.

@@ -1,0 +1,348 @@
+// Host-side bookkeeping of the operators on the K/V cache: which slot holds
+// each 64-position tile of each sequence, the order in which a copy moves
+// tiles, and the launch shape of attention over tiles that sequences share.
+// Plain arithmetic with no HIP types, so the same code also builds for the CPU
+// alone (the host checks under tests/).
+#pragma once
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+#include <cstring>
+#include <vector>
+
+constexpr int kTile = 64;       // positions per tile
+constexpr int kMaxSlots = 256;  // sequences of a cache (RV_MAX_BATCH)
+
+// ---------------------------------------------------------------- ownership
+// Tile t of sequence b lies in the slot of sequence at(b, t): its own unless b
+// was forked from a sequence whose tile it reads.  A tile is only ever read at
+// its own index t, so a slot's number says where it lies.  A sequence writes
+// only to tiles of its own slot that no other sequence reads.
+struct TileOwners {
+  int B = 0, T = 0;
+  int foreign = 0;             // (b, t) with at(b, t) != b
+  std::vector<uint8_t> own;    // [B][T]
+  std::vector<uint16_t> refs;  // [B][T]: other sequences that read tile t of slot b
+
+  void create(int batch, int tiles) {
+    B = batch;
+    T = tiles;
+    own.resize((size_t)B * T);
+    refs.resize((size_t)B * T);
+    reset();
+  }
+  void reset() {
+    foreign = 0;
+    for (int b = 0; b < B; ++b) std::fill_n(own.begin() + (size_t)b * T, T, (uint8_t)b);
+    std::fill(refs.begin(), refs.end(), (uint16_t)0);
+  }
+  int at(int b, int t) const { return own[(size_t)b * T + t]; }
+  void set(int b, int t, int slot) {
+    uint8_t& o = own[(size_t)b * T + t];
+    if (o != b) {
+      --refs[(size_t)o * T + t];
+      --foreign;
+    }
+    o = (uint8_t)slot;
+    if (slot != b) {
+      ++refs[(size_t)slot * T + t];
+      ++foreign;
+    }
+  }
+  void make_private(int b) {
+    for (int t = 0; foreign && t < T; ++t) set(b, t, b);
+  }
+  bool private_row(int b) const {
+    const uint8_t* o = own.data() + (size_t)b * T;
+    for (int t = 0; t < T; ++t)
+      if (o[t] != b) return false;
+    return true;
+  }
+  // First tile of [t0, t1) that b may not write (-1: none).
+  int first_shared(int b, int t0, int t1) const {
+    if (!foreign) return -1;
+    for (int t = t0; t < t1; ++t)
+      if (at(b, t) != b || refs[(size_t)b * T + t]) return t;
+    return -1;
+  }
+  // A sequence outside `gone` that reads a tile of a slot in it, or -1.
+  int reader_of(const bool* gone) const {
+    if (!foreign) return -1;
+    for (int b = 0; b < B; ++b) {
+      if (gone[b]) continue;
+      for (int t = 0; t < T; ++t)
+        if (gone[at(b, t)]) return b;
+    }
+    return -1;
+  }
+  // Leading tiles, at most cap, that a and b read from the same slots.
+  int common(int a, int b, int cap) const {
+    const uint8_t *x = own.data() + (size_t)a * T, *y = own.data() + (size_t)b * T;
+    int t = 0;
+    for (; t + 8 <= cap; t += 8) {
+      uint64_t u, v;
+      memcpy(&u, x + t, 8);
+      memcpy(&v, y + t, 8);
+      if (u != v) break;
+    }
+    while (t < cap && x[t] == y[t]) ++t;
+    return t;
+  }
+};
+
+// ---------------------------------------------------------------- copying
+// Moves between slots that all read what was there before any of them wrote.
+// A unit is a list of moves that one thread executes in order, batch of
+// kMoveBatch by batch (it reads the whole batch before it writes it); different
+// units touch no slot that another writes.  The order within a unit:
+// a slot is overwritten once every move that reads it has been executed; what
+// then remains is one cycle, which is opened by saving the slot that its first
+// move overwrites, for its last move (from_saved) to write.
+constexpr int kMoveBatch = 4;
+constexpr int kFanMoves = 8;  // moves of one source per unit where nothing overwrites it
+
+struct CopyProgram {
+  int n = 0, units = 0;
+  uint8_t src[kMaxSlots], dst[kMaxSlots];
+  int32_t len[kMaxSlots];
+  uint8_t from_saved[kMaxSlots];
+  int16_t unit0[kMaxSlots + 1];   // first move of each unit
+  int16_t saved[kMaxSlots];       // slot that the unit saves at its start, or -1
+};
+
+// h_src / h_dst: slots of the moves (destinations distinct), h_len what each brings.
+inline void plan_copy(int n, const uint8_t* h_src, const uint8_t* h_dst, const int32_t* h_len, CopyProgram& p) {
+  int16_t mover[kMaxSlots], readers[kMaxSlots], parent[kMaxSlots];
+  for (int s = 0; s < kMaxSlots; ++s) {
+    mover[s] = -1;
+    readers[s] = 0;
+    parent[s] = (int16_t)s;
+  }
+  auto root = [&](int s) {
+    while (parent[s] != s) s = parent[s] = parent[parent[s]];
+    return s;
+  };
+  for (int i = 0; i < n; ++i)
+    if (h_src[i] != h_dst[i]) mover[h_dst[i]] = (int16_t)i;
+  for (int i = 0; i < n; ++i) {
+    if (h_src[i] == h_dst[i]) continue;
+    ++readers[h_src[i]];
+    if (mover[h_src[i]] >= 0) parent[root(h_src[i])] = (int16_t)root(h_dst[i]);  // must be ordered
+  }
+  // a source that is overwritten ties together every move that reads it (above);
+  // one that is not leaves its moves free
+  p.n = p.units = 0;
+  int16_t open_saved = -1;
+  int unit_first = 0;
+  auto close = [&]() {
+    if (p.n == unit_first) return;
+    p.unit0[p.units] = (int16_t)unit_first;
+    p.saved[p.units] = open_saved;
+    ++p.units;
+    unit_first = p.n;
+    open_saved = -1;
+  };
+  auto push = [&](int i, bool from_saved) {
+    p.src[p.n] = h_src[i];
+    p.dst[p.n] = h_dst[i];
+    p.len[p.n] = h_len[i];
+    p.from_saved[p.n] = from_saved;
+    ++p.n;
+  };
+  // free moves: by source, in units of up to kFanMoves
+  bool done[kMaxSlots];
+  for (int i = 0; i < n; ++i) done[i] = h_src[i] == h_dst[i];
+  for (int i = 0; i < n; ++i) {
+    if (done[i] || mover[h_src[i]] >= 0 || readers[h_dst[i]]) continue;
+    for (int j = i; j < n; ++j) {
+      if (done[j] || h_src[j] != h_src[i] || readers[h_dst[j]]) continue;
+      push(j, false);
+      done[j] = true;
+      if (p.n - unit_first == kFanMoves) close();
+    }
+    close();
+  }
+  // ordered moves: one unit per set of slots tied together
+  for (int r = 0; r < kMaxSlots; ++r) {
+    if (root(r) != r) continue;
+    bool again = true;
+    while (again) {  // moves whose destination nothing still reads
+      again = false;
+      for (int i = 0; i < n; ++i) {
+        if (done[i] || root(h_dst[i]) != r || readers[h_dst[i]]) continue;
+        push(i, false);
+        done[i] = true;
+        --readers[h_src[i]];
+        again = true;
+      }
+    }
+    for (int i = 0; i < n; ++i) {
+      if (done[i] || root(h_dst[i]) != r) continue;
+      // the rest is one cycle: dst(i) <- src(i) <- ... <- dst(i)
+      open_saved = h_dst[i];
+      for (int j = i;;) {
+        done[j] = true;
+        const int next = mover[h_src[j]];
+        push(j, next == i);
+        if (next == i) break;
+        j = next;
+      }
+      break;
+    }
+    close();
+  }
+  p.unit0[p.units] = (int16_t)p.n;
+}
+
+// ---------------------------------------------------------------- attention
+// Query rows of one call: sequence b has rows row0[b] .. row0[b+1]-1 at
+// positions pos0[b] ...  Sequences that read the same leading tiles form a
+// group; its shared keys 0 .. 64*tiles-1 lie before every row of it, and are
+// attended by the queries of all its rows together (one query slot for each
+// (member, row < rmax, head of the kv head), so slots of a member with fewer
+// rows stay empty).  Every sequence then attends its remaining keys alone.
+// Both parts are split into runs of keys; the results of a row's runs (slots
+// 0 .. sh.ns-1 of the shared part, then those of its own) are merged afterwards.
+constexpr int kShareGroups = 32;
+constexpr int kMergeSlots = 96;
+
+struct SharePart {
+  int qpw = 0;   // queries per workgroup
+  int nqg = 0;   // query groups of the largest unit
+  int ks = 0;    // keys per run (multiple of 64)
+  int ns = 0;    // runs of the longest unit
+};
+
+struct SharePlan {
+  int nseq = 0, rows = 0, groups = 0;
+  SharePart sh, own;
+  uint8_t group_of[kMaxSlots];   // 255: none
+  uint8_t member[kMaxSlots];     // members, group after group
+  int16_t first[kShareGroups + 1];
+  int32_t tiles[kShareGroups], rmax[kShareGroups];
+  int slots() const { return (groups ? sh.ns : 0) + own.ns; }
+};
+
+// Groups of sequences that share leading tiles (all tables as described above).
+// A sequence belongs to the group that saves the most tile reads among those
+// still free; slots of a group count at most twice its queries.
+inline void plan_groups(const TileOwners& tl, const int32_t* pos0, const int32_t* row0, SharePlan& p) {
+  const int B = tl.B;
+  p.groups = 0;
+  p.first[0] = 0;
+  memset(p.group_of, 255, sizeof p.group_of);
+  if (!tl.foreign) return;
+  bool free_[kMaxSlots];
+  for (int b = 0; b < B; ++b) free_[b] = row0[b + 1] > row0[b] && pos0[b] >= kTile;
+  for (int b = 0; b < B && p.groups < kShareGroups; ++b) {
+    if (!free_[b]) continue;
+    // leading tiles that each free sequence has in common with b
+    int c[kMaxSlots], order[kMaxSlots], m = 0;
+    for (int x = b; x < B; ++x) {
+      if (!free_[x] || tl.at(x, 0) != tl.at(b, 0)) continue;
+      c[x] = tl.common(b, x, std::min(pos0[b], pos0[x]) / kTile);
+      if (c[x] > 0) order[m++] = x;
+    }
+    if (m < 2) continue;
+    std::sort(order, order + m, [&](int x, int y) { return c[x] != c[y] ? c[x] > c[y] : x < y; });
+    long long best = 0;
+    int take = 0;
+    for (int i = 1; i < m; ++i)
+      if ((long long)c[order[i]] * i > best) {
+        best = (long long)c[order[i]] * i;
+        take = i + 1;
+      }
+    long long sum = 0;
+    int rmax = 0;
+    for (int i = 0; i < take; ++i) {
+      const int r = row0[order[i] + 1] - row0[order[i]];
+      sum += r;
+      rmax = std::max(rmax, r);
+    }
+    if ((long long)take * rmax > 2 * sum) continue;
+    const int g = p.groups++, f = p.first[g];
+    p.tiles[g] = c[order[take - 1]];
+    p.rmax[g] = rmax;
+    std::sort(order, order + take);
+    for (int i = 0; i < take; ++i) {
+      p.member[f + i] = (uint8_t)order[i];
+      p.group_of[order[i]] = (uint8_t)g;
+      free_[order[i]] = false;
+    }
+    p.first[g + 1] = (int16_t)(f + take);
+  }
+}
+
+// One unit of a part: `keys` keys against `queries` queries of a kv head.
+struct ShareUnit {
+  int keys, queries;
+};
+
+// Run length of one part: the cheapest estimate over a few run counts, within
+// max_ns runs.  One run only where `single` asks for the whole part in one.
+inline SharePart plan_part(bool bf16, const ShareUnit* u, int n, int n_kv, int hd, int max_ns) {
+  SharePart s;
+  int kmax = 0, qmax = 0;
+  for (int i = 0; i < n; ++i) {
+    kmax = std::max(kmax, u[i].keys);
+    qmax = std::max(qmax, u[i].queries);
+  }
+  if (!kmax || !qmax) return s;
+  s.qpw = !bf16 || qmax <= 16 ? 16 : 128;
+  s.nqg = (qmax + s.qpw - 1) / s.qpw;
+  static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80};
+  double best = 0;
+  for (int ns : counts) {
+    if (ns > max_ns || (ns > 1 && (ns - 1) * kTile >= kmax)) break;
+    const int ks = ((kmax + ns - 1) / ns + kTile - 1) / kTile * kTile;
+    long long wgs = 0, keys = 0;
+    for (int i = 0; i < n; ++i) {
+      wgs += (long long)((u[i].keys + ks - 1) / ks) * ((u[i].queries + s.qpw - 1) / s.qpw) * n_kv;
+      keys += u[i].keys;
+    }
+    double t;
+    if (!bf16) {  // a wave per workgroup, eight resident on a CU
+      t = (double)((wgs + 2047) / 2048) * (ks / kTile + 1) * 3.0 * hd / 128;
+    } else if (s.qpw == 16) {
+      const double stream = (double)keys * n_kv * 8 * hd / 5.5e6;
+      t = std::max((double)((wgs + 255) / 256) * std::min(ks, kmax) * 8 * hd / 4.5e4, stream);
+    } else {
+      t = (double)((wgs + 255) / 256) * (ks / kTile + 2) * 2.9 * hd / 128;
+    }
+    const int runs = (kmax + ks - 1) / ks;
+    t += 0.05 * runs;
+    if (!s.ks || t < best) {
+      best = t;
+      s.ks = ks;
+      s.ns = runs;
+    }
+  }
+  return s;
+}
+
+// Launch shape of a call.  part_entries: (slot, row, head) results that the
+// partial buffer holds; n_heads * rows <= part_entries / 2 always fits.
+inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, const int32_t* row0, int n_heads, int n_kv,
+                       int hd, size_t part_entries, SharePlan& p) {
+  const int B = tl.B, G = n_heads / n_kv;
+  p.nseq = B;
+  p.rows = row0[B];
+  plan_groups(tl, pos0, row0, p);
+  const int fit = (int)std::min<size_t>(kMergeSlots, part_entries / ((size_t)p.rows * n_heads));
+  ShareUnit u[kMaxSlots];
+  int n = 0;
+  p.sh = SharePart{};
+  if (p.groups) {
+    for (int g = 0; g < p.groups; ++g)
+      u[n++] = ShareUnit{p.tiles[g] * kTile, (p.first[g + 1] - p.first[g]) * p.rmax[g] * G};
+    p.sh = plan_part(bf16, u, n, n_kv, hd, std::max(1, fit / 2));
+  }
+  n = 0;
+  for (int b = 0; b < B; ++b) {
+    const int r = row0[b + 1] - row0[b];
+    if (!r) continue;
+    const int t0 = p.group_of[b] == 255 ? 0 : p.tiles[p.group_of[b]];
+    u[n++] = ShareUnit{pos0[b] + r - t0 * kTile, r * G};
+  }
+  p.own = plan_part(bf16, u, n, n_kv, hd, std::max(1, fit - p.sh.ns));
+}

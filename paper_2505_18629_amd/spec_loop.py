@@ -56,6 +56,13 @@ class SpeculativeLoop:
         self.tokens = [list(map(int, p)) for p in prefixes]
         return self.lens
 
+    def prefill_shared(self, prefix: Sequence[int]):
+        """One prompt for every sequence, computed once in each model and forked (rv_cache_fork)."""
+        self.lens = self.target.prefill_shared(prefix)
+        self.draft.prefill_shared(prefix)
+        self.tokens = [list(map(int, prefix)) for _ in range(self.target.batch)]
+        return self.lens
+
     def _round_seed(self, j: int) -> int:
         return ((self.seed & 0xFFFFFFFF) << 32) | ((self.rounds * (self.k + 1) + j) & 0xFFFFFFFF)
 
