@@ -240,29 +240,28 @@ rv_status rv_fuse_accept_noalloc(const float* d_logits, int32_t batch, int32_t k
  * copied or forked, and query rows attend a layer.  rv_verify* on a forked cache
  * attends the same way.
  *
- * A call on rows takes two host arrays: sequence b has h_rows[b] rows (0 for
- * none) at positions h_pos[b] .. h_pos[b] + h_rows[b] - 1, all below max_len
- * (else RV_E_RANGE); the rows of the batch follow each other, sequence after
- * sequence.  A row is n heads x head_dim values of RV_F32 or RV_BF16, whatever
- * the model's type; rows start at multiples of 16 bytes, `ld` elements apart.
- * Calls on one cache share its workspace and its tables: they, and graphs that
- * hold them, must not overlap (as for rv_verify).  Host arrays are read before
- * the call returns; a captured call keeps the values it was captured with, also
- * those of the cache's tiles, so a graph is captured anew after a fork, a copy or
- * a prefill that changes which tiles are shared. */
+ * A call on rows takes two host arrays of `batch` entries (the cache's batch, else
+ * RV_E_ARG): sequence b has h_rows[b] rows (0 for none) at positions h_pos[b] ..
+ * h_pos[b] + h_rows[b] - 1, all below max_len (else RV_E_RANGE); the n_rows rows
+ * of the batch follow each other, sequence after sequence.  A row is heads x
+ * head_dim values of RV_F32 or RV_BF16, whatever the model's type; rows start at
+ * multiples of 16 bytes, `ld` elements apart.  n_rows and the widths say what the
+ * caller's memory holds and must be what the counts and the model need (else
+ * RV_E_ARG).  Calls on one cache share its workspace and its tables: they, and
+ * graphs that hold them, must not overlap (as for rv_verify).  Host arrays are
+ * read before the call returns; a captured call keeps the values it was captured
+ * with, also which tiles are shared, so a graph is captured anew after a fork,
+ * copy or prefill that changes that. */
 
 typedef struct {
   int32_t dtype;                      /* of all rows: RV_F32 or RV_BF16 */
   int32_t rotate;                     /* 0: keys (and queries) are stored as they are */
-  const void *d_q, *d_k, *d_v;        /* n_heads, n_kv_heads, n_kv_heads heads; d_q may be NULL */
-  int64_t ld_q, ld_k, ld_v;
+  int64_t n_rows, q_width, kv_width;  /* q_width: n_heads * head_dim, or 0 without queries */
+  const void *d_q, *d_k, *d_v;        /* d_q may be NULL */
   void* d_q_out;                      /* queries, normalised and rotated; may be d_q; NULL with d_q */
-  int64_t ld_q_out;
+  int64_t ld_q, ld_k, ld_v, ld_q_out;
   const float *d_q_gain, *d_k_gain;   /* [head_dim] fp32, or NULL: that side is not normalised */
 } rv_rows;
-
-/* What the rows of a call must fit: h_dims[0..3] = batch, n_heads, n_kv_heads, head_dim. */
-rv_status rv_cache_dims(const rv_cache* c, int32_t* h_dims);
 
 /* Writes rows of K and V to one layer of the cache.  With gains, each head x of
  * a query or key is first normalised, y = x / sqrt(mean(x^2) + rms_eps) * g;
@@ -270,12 +269,13 @@ rv_status rv_cache_dims(const rv_cache* c, int32_t* h_dims);
  * in the pass).  Rows of the sequence at other positions stay as they are, and so
  * does the id history.  RV_E_STATE for positions of a tile that another sequence
  * shares (rv_cache_fork).  Asynchronous. */
-rv_status rv_cache_append(rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows,
+rv_status rv_cache_append(rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
                           const rv_rows* rows, void* stream);
 
 /* Reads K and V rows of one layer back as values (hi + lo for bf16 models). */
-rv_status rv_cache_read(const rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows, int32_t dtype,
-                        void* d_k, int64_t ld_k, void* d_v, int64_t ld_v, void* stream);
+rv_status rv_cache_read(const rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
+                        int32_t dtype, int64_t n_rows, int64_t width, void* d_k, int64_t ld_k, void* d_v, int64_t ld_v,
+                        void* stream);
 
 /* Copies sequences: h_dst[i] becomes what h_src[i] was before the call, up to
  * its first h_len[i] committed tokens: ids 0 .. len-1 and, in every layer, K and
@@ -304,8 +304,9 @@ rv_status rv_cache_fork(rv_cache* c, int32_t src, int32_t len, int32_t n, const 
  * n_kv_heads).  Tiles that several sequences of the call share are read once for
  * all their rows.  At most as many rows as the workspace holds: max(batch *
  * max_block, 2048) (else RV_E_CAPACITY).  d_out may be d_q.  Asynchronous. */
-rv_status rv_cache_attend(const rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows, int32_t dtype,
-                          const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* stream);
+rv_status rv_cache_attend(const rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
+                          int32_t dtype, int64_t n_rows, int64_t width, const void* d_q, int64_t ld_q, void* d_out,
+                          int64_t ld_out, void* stream);
 
 /* From now on the passes of this model normalise queries and keys for each head
  * before the rotation (as rv_cache_append does), with gains [n_layers][head_dim]

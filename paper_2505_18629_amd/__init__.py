@@ -66,9 +66,10 @@ class rv_fusion(ctypes.Structure):
 
 
 class rv_rows(ctypes.Structure):
-    _fields_ = [("dtype", ctypes.c_int32), ("rotate", ctypes.c_int32), ("d_q", ctypes.c_void_p),
-                ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("ld_q", ctypes.c_int64),
-                ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("d_q_out", ctypes.c_void_p),
+    _fields_ = [("dtype", ctypes.c_int32), ("rotate", ctypes.c_int32), ("n_rows", ctypes.c_int64),
+                ("q_width", ctypes.c_int64), ("kv_width", ctypes.c_int64), ("d_q", ctypes.c_void_p),
+                ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_q_out", ctypes.c_void_p),
+                ("ld_q", ctypes.c_int64), ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64),
                 ("ld_q_out", ctypes.c_int64), ("d_q_gain", ctypes.c_void_p), ("d_k_gain", ctypes.c_void_p)]
 
 
@@ -81,6 +82,7 @@ class RVError(RuntimeError):
 
 _vp, _i32, _i64, _u64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t
 _P_i32 = ctypes.POINTER(ctypes.c_int32)
+_cp = ctypes.c_char_p  # host arrays handed over as bytes
 _sig = {
     "rv_status_str": ([ctypes.c_int], ctypes.c_char_p),
     "rv_last_error": ([], ctypes.c_char_p),
@@ -98,11 +100,11 @@ _sig = {
     "rv_verify_ragged": ([_vp, _P_i32, _vp, _i32, _P_i32, _vp, _i32, ctypes.POINTER(rv_fusion), _vp, _vp, _vp],
                          ctypes.c_int),
     "rv_fuse_accept_noalloc": ([_vp, _i32, _i32, _i32, _vp, ctypes.POINTER(rv_fusion), _vp, _vp, _vp], ctypes.c_int),
-    "rv_cache_append": ([_vp, _i32, _vp, _vp, ctypes.POINTER(rv_rows), _vp], ctypes.c_int),
-    "rv_cache_read": ([_vp, _i32, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
-    "rv_cache_copy": ([_vp, _i32, _vp, _vp, _vp, _vp], ctypes.c_int),
-    "rv_cache_fork": ([_vp, _i32, _i32, _i32, _vp, _vp], ctypes.c_int),
-    "rv_cache_attend": ([_vp, _i32, _vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
+    "rv_cache_append": ([_vp, _i32, _i32, _cp, _cp, ctypes.POINTER(rv_rows), _vp], ctypes.c_int),
+    "rv_cache_read": ([_vp, _i32, _i32, _cp, _cp, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
+    "rv_cache_copy": ([_vp, _i32, _cp, _cp, _cp, _vp], ctypes.c_int),
+    "rv_cache_fork": ([_vp, _i32, _i32, _i32, _cp, _vp], ctypes.c_int),
+    "rv_cache_attend": ([_vp, _i32, _i32, _cp, _cp, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
     "rv_cache_dims": ([_vp, _vp], ctypes.c_int),
     "rv_model_qk_norm": ([_vp, _vp, _vp], ctypes.c_int),
     "rv_debug_cache_span": ([_vp, _i32, ctypes.POINTER(_sz), ctypes.POINTER(_sz)], ctypes.c_int),
@@ -262,15 +264,45 @@ def rv_fuse_accept_noalloc(logits, k: int, draft_ids, alpha: float, accept_len, 
 _ROW_TYPES = {torch.float32: RV_F32, torch.bfloat16: RV_BF16}
 
 
-def _i32_array(vals, n: Optional[int] = None) -> np.ndarray:
+def _i32_bytes(vals):
+    """(entries, their bytes) of a list of whole numbers."""
     arr = np.ascontiguousarray(vals, dtype=np.int32)
-    if arr.ndim != 1 or (n is not None and arr.size != n):
-        raise ValueError(f"expected {'a list' if n is None else n} of whole numbers, got shape {arr.shape}")
-    return arr
+    if arr.ndim != 1:
+        raise ValueError(f"expected a list of whole numbers, got shape {arr.shape}")
+    return arr.size, arr.tobytes()
 
 
-def _addr(arr: np.ndarray) -> int:
-    return arr.__array_interface__["data"][0]
+def _spans(positions, counts):
+    batch, pos = _i32_bytes(positions)
+    size, n = _i32_bytes(counts)
+    if size != batch:
+        raise ValueError(f"{batch} positions and {size} counts")
+    return batch, pos, n
+
+
+def _row_tensors(a, *others) -> int:
+    """Type of the rows of tensors of one type on the current device, each dense within a row."""
+    kind = _ROW_TYPES.get(a.dtype)
+    if kind is None:
+        raise ValueError(f"rows must be float32 or bfloat16, not {a.dtype}")
+    here, rows = torch.cuda.current_device(), a.shape[0]
+    for t in (a,) + others:
+        if t.dim() != 2 or t.shape[0] != rows or t.dtype != a.dtype or (t.stride(1) != 1 and rows):
+            raise ValueError(f"expected {rows} rows of {a.dtype}, dense within a row, got {tuple(t.shape)} of {t.dtype} "
+                             f"with strides {t.stride()}")
+        if t.get_device() != here:
+            raise ValueError(f"rows on {t.device}, the current device is cuda:{here}")
+    return kind
+
+
+def _gain(t, hd: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (hd,) or not t.is_contiguous() or \
+            t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"gains must be {hd} contiguous float32 values on the current device, got {tuple(t.shape)} of "
+                         f"{t.dtype} on {t.device}")
+    return t.data_ptr()
 
 
 def rv_cache_dims(cache: int):
@@ -280,72 +312,53 @@ def rv_cache_dims(cache: int):
     return tuple(d)
 
 
-def _spans(batch: int, positions, counts):
-    pos, n = _i32_array(positions, batch), _i32_array(counts, batch)
-    return pos, n, int(n.sum())
-
-
-def _row_type(total: int, *rows) -> int:
-    """Type of the rows; each (tensor, width) given holds `total` rows of one type on the current device."""
-    dtype, here = rows[0][0].dtype, torch.cuda.current_device()
-    if dtype not in _ROW_TYPES:
-        raise ValueError(f"rows must be float32 or bfloat16, not {dtype}")
-    for t, width in rows:
-        if tuple(t.shape) != (total, width) or t.dtype != dtype or (total and t.stride(1) != 1):
-            raise ValueError(f"expected {total} rows of {width} {dtype}, dense within a row, got {tuple(t.shape)} of "
-                             f"{t.dtype} with strides {t.stride()}")
-        if not t.is_cuda or t.device.index != here:
-            raise ValueError(f"rows on {t.device}, the current device is cuda:{here}")
-    return _ROW_TYPES[dtype]
-
-
-def _gain(t, shape) -> Optional[int]:
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"gains must be contiguous float32 {shape}, got {tuple(t.shape)} of {t.dtype}")
-    return _dev(t)
-
-
 def rv_cache_append(cache: int, layer: int, positions, counts, q, k, v, q_out, q_gain=None, k_gain=None,
                     rotate: bool = True, stream=None) -> None:
     """q and q_out may be None together; q_out may be q."""
-    batch, hq, hkv, hd = rv_cache_dims(cache)
-    pos, n, total = _spans(batch, positions, counts)
-    rows = [(k, hkv * hd), (v, hkv * hd)] + [(t, hq * hd) for t in (q, q_out) if t is not None]
-    kind = _row_type(total, *rows)
-    a = rv_rows(kind, 1 if rotate else 0, _dev(q), _dev(k), _dev(v), 0 if q is None else q.stride(0), k.stride(0),
-                v.stride(0), _dev(q_out), 0 if q_out is None else q_out.stride(0), _gain(q_gain, (hd,)),
-                _gain(k_gain, (hd,)))
-    _check(_lib.rv_cache_append(cache, layer, _addr(pos), _addr(n), ctypes.byref(a), _stream(stream)))
+    batch, pos, n = _spans(positions, counts)
+    rows, width = k.shape
+    if v.shape != k.shape or (q is None) != (q_out is None) or (q is not None and q.shape != q_out.shape):
+        raise ValueError("k and v, and q and its output, have the same shape")
+    hd = 0 if q_gain is None and k_gain is None else rv_cache_dims(cache)[3]
+    if q is None:
+        a = rv_rows(_row_tensors(k, v), rotate, rows, 0, width, None, k.data_ptr(), v.data_ptr(), None, 0, k.stride(0),
+                    v.stride(0), 0, _gain(q_gain, hd), _gain(k_gain, hd))
+    else:
+        a = rv_rows(_row_tensors(k, v, q, q_out), rotate, rows, q.shape[1], width, q.data_ptr(), k.data_ptr(),
+                    v.data_ptr(), q_out.data_ptr(), q.stride(0), k.stride(0), v.stride(0), q_out.stride(0),
+                    _gain(q_gain, hd), _gain(k_gain, hd))
+    _check(_lib.rv_cache_append(cache, layer, batch, pos, n, ctypes.byref(a), _stream(stream)))
 
 
 def rv_cache_read(cache: int, layer: int, positions, counts, k, v, stream=None) -> None:
-    batch, _, hkv, hd = rv_cache_dims(cache)
-    pos, n, total = _spans(batch, positions, counts)
-    kind = _row_type(total, (k, hkv * hd), (v, hkv * hd))
-    _check(_lib.rv_cache_read(cache, layer, _addr(pos), _addr(n), kind, _dev(k), k.stride(0), _dev(v), v.stride(0),
-                              _stream(stream)))
+    batch, pos, n = _spans(positions, counts)
+    if v.shape != k.shape:
+        raise ValueError("k and v have the same shape")
+    kind = _row_tensors(k, v)
+    _check(_lib.rv_cache_read(cache, layer, batch, pos, n, kind, k.shape[0], k.shape[1], k.data_ptr(), k.stride(0),
+                              v.data_ptr(), v.stride(0), _stream(stream)))
 
 
 def rv_cache_copy(cache: int, src, dst, lengths, stream=None) -> None:
-    s = _i32_array(src)
-    d, n = _i32_array(dst, s.size), _i32_array(lengths, s.size)
-    _check(_lib.rv_cache_copy(cache, s.size, _addr(s), _addr(d), _addr(n), _stream(stream)))
+    (a, s), (b, d), (c, n) = _i32_bytes(src), _i32_bytes(dst), _i32_bytes(lengths)
+    if a != b or a != c:
+        raise ValueError(f"{a} sources, {b} destinations and {c} lengths")
+    _check(_lib.rv_cache_copy(cache, a, s, d, n, _stream(stream)))
 
 
 def rv_cache_fork(cache: int, src: int, length: int, dst, stream=None) -> None:
-    d = _i32_array(dst)
-    _check(_lib.rv_cache_fork(cache, src, length, d.size, _addr(d), _stream(stream)))
+    n, d = _i32_bytes(dst)
+    _check(_lib.rv_cache_fork(cache, src, length, n, d, _stream(stream)))
 
 
 def rv_cache_attend(cache: int, layer: int, positions, counts, q, out, stream=None) -> None:
     """out may be q."""
-    batch, hq, _, hd = rv_cache_dims(cache)
-    pos, n, total = _spans(batch, positions, counts)
-    kind = _row_type(total, (q, hq * hd), (out, hq * hd))
-    _check(_lib.rv_cache_attend(cache, layer, _addr(pos), _addr(n), kind, _dev(q), q.stride(0), _dev(out),
-                                out.stride(0), _stream(stream)))
+    batch, pos, n = _spans(positions, counts)
+    if out.shape != q.shape:
+        raise ValueError("q and the output have the same shape")
+    kind = _row_tensors(q, out)
+    _check(_lib.rv_cache_attend(cache, layer, batch, pos, n, kind, q.shape[0], q.shape[1], q.data_ptr(), q.stride(0),
+                                out.data_ptr(), out.stride(0), _stream(stream)))
 
 
 def rv_model_qk_norm(model: int, q_gain, k_gain) -> None:

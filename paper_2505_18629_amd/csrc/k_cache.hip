@@ -69,6 +69,11 @@ RV_DEV void load_pair8(const void* hi, const void* lo, size_t i, float (&x)[8]) 
   for (int j = 0; j < 8; ++j) x[j] += l[j];
 }
 
+// Whether keys [k_lo, k_hi) of a V block hold any of slot group g's.
+RV_DEV bool group_touched(int g, int k_lo, int k_hi) {
+  return (4 * g < k_hi && 4 * g + 4 > k_lo) || (16 + 4 * g < k_hi && 20 + 4 * g > k_lo);
+}
+
 // ----------------------------------------------------------- append
 // Row r of sequence b at position p = pos[b] + r, per head of q and k:
 //   y = x / sqrt(mean(x^2) + eps) * g              (with gains)
@@ -76,14 +81,18 @@ RV_DEV void load_pair8(const void* hi, const void* lo, size_t i, float (&x)[8]) 
 // with c, s of the angle p base^(-2i/hd) from the cache's rotary table; q goes
 // to q_out, k and v to the cache.  Statistics and rotation are fp32.
 //
-// One workgroup per (32-position block of a sequence, `hpw` heads of the list
-// q heads, k heads, v heads).  hd / 16 threads per (row, head) own dims d..d+7
-// and their partners d+hd/2..: 16-byte loads and stores throughout, the norm is
-// a sum over those threads, and rows are adjacent in a wave, so that a K
-// unit of the bf16 cache (16 positions x 32 dims) is written whole.  A V unit holds 8
-// positions of one dim: rows go through LDS and each thread writes the 8
-// positions of a (dim, slot group) with one store -- 2-byte stores of single
-// positions remain for the groups that the rows fill in part.
+// Workgroups: (32-position block of a sequence) x (hpw q or k heads, or one v
+// head).  hd / 16 threads per (row, head) own dims d..d+7 and their partners
+// d+hd/2..: 16-byte loads and stores throughout, the norm is a sum over those
+// threads, and rows are adjacent in a wave, so that a K unit of the bf16 cache
+// (16 positions x 32 dims) is written whole.  A thread keeps its row's rotary
+// factors for kHeadBatch heads whose loads it issues together (one head per
+// workgroup reads as many bytes of factors as of rows: 38 us for 4.1k ragged
+// rows of 32/8 heads x 128 in bf16).  A V unit holds 8 positions of one dim:
+// rows go through LDS and each thread writes the 8 positions of a (dim, slot
+// group) with one store -- 2-byte stores of single positions remain for the
+// groups that the rows fill in part.
+constexpr int kHeadBatch = 4;
 template <int DT, int IO, int HD>
 __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   constexpr int HALF = HD / 2, TPH = HD / 16;  // threads per (row, head)
@@ -94,103 +103,123 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   const int p_lo = max(pos0, blk * kBlockPos), p_hi = min(pos0 + n, (blk + 1) * kBlockPos);
   const int rows = p_hi - p_lo, row_lo = a.row0[b] + (p_lo - pos0);
   const int tid = threadIdx.x;
-  const int h_lo = blockIdx.y * a.hpw, h_end = min(h_lo + a.hpw, a.n_heads + 2 * a.n_kv);
   const int n_qk = a.n_heads + a.n_kv;
 
-  // q and k heads: thread -> (head, row, part), parts fastest, then rows
-  const int qk_end = min(h_end, n_qk), per_head = rows * TPH;
-  for (int i = tid; i < (qk_end - h_lo) * per_head; i += 256) {
-    const int h = h_lo + i / per_head, r = i % per_head / TPH, d = i % TPH * 8;
-    const bool is_q = h < a.n_heads;
-    const int hh = is_q ? h : h - a.n_heads, p = p_lo + r;
-    const void* src = is_q ? a.q : a.k;
-    const size_t at = (size_t)(row_lo + r) * (is_q ? a.ldq : a.ldk) + (size_t)hh * HD + d;
-    float y1[8], y2[8];
-    load8<IO>(src, at, y1);
-    load8<IO>(src, at + HALF, y2);
-    const float* gain = is_q ? a.q_gain : a.k_gain;
-    if (gain) {
-      float ss = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ss += y1[j] * y1[j] + y2[j] * y2[j];
-#pragma unroll
-      for (int m = 1; m < TPH; m *= 2) ss += __shfl_xor(ss, m, 64);
-      const float rs = 1.0f / sqrtf(ss / (float)HD + a.eps);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        y1[j] = y1[j] * rs * gain[d + j];
-        y2[j] = y2[j] * rs * gain[HALF + d + j];
-      }
-    }
+  // q and k heads: thread -> (head of the batch's first, row, part), parts fastest, then rows
+  if ((int)blockIdx.y < a.qk_groups) {
+    const int h_lo = blockIdx.y * a.hpw, h_end = min(h_lo + a.hpw, n_qk);
+    const int per_head = rows * TPH, par = 256 / per_head;  // heads side by side
+    if (tid >= par * per_head) return;
+    const int r = tid % per_head / TPH, d = tid % TPH * 8, p = p_lo + r;
+    float cs[8], sn[8], gq1[8], gq2[8], gk1[8], gk2[8];
     if (a.rotate) {
-      float cs[8], sn[8];
       load8<RV_F32>(a.rope_cos, (size_t)p * HALF + d, cs);
       load8<RV_F32>(a.rope_sin, (size_t)p * HALF + d, sn);
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float u = y1[j], v = y2[j];
-        y1[j] = u * cs[j] - v * sn[j];
-        y2[j] = v * cs[j] + u * sn[j];
+    for (int j = 0; j < 8; ++j) {
+      gq1[j] = a.q_gain ? a.q_gain[d + j] : 0.f;
+      gq2[j] = a.q_gain ? a.q_gain[HALF + d + j] : 0.f;
+      gk1[j] = a.k_gain ? a.k_gain[d + j] : 0.f;
+      gk2[j] = a.k_gain ? a.k_gain[HALF + d + j] : 0.f;
+    }
+    for (int h0 = h_lo + tid / per_head; h0 < h_end; h0 += kHeadBatch * par) {
+      float y1[kHeadBatch][8], y2[kHeadBatch][8];
+#pragma unroll
+      for (int u = 0; u < kHeadBatch; ++u) {
+        const int h = min(h0 + u * par, h_end - 1);  // past the last: that one again, not stored
+        const bool is_q = h < a.n_heads;
+        const void* src = is_q ? a.q : a.k;
+        const size_t at = (size_t)(row_lo + r) * (is_q ? a.ldq : a.ldk) + (size_t)(is_q ? h : h - a.n_heads) * HD + d;
+        load8<IO>(src, at, y1[u]);
+        load8<IO>(src, at + HALF, y2[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kHeadBatch; ++u) {
+        const int h = h0 + u * par;
+        if (h >= h_end) break;
+        const bool is_q = h < a.n_heads;
+        const int hh = is_q ? h : h - a.n_heads;
+        if (is_q ? a.q_gain : a.k_gain) {
+          float ss = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) ss += y1[u][j] * y1[u][j] + y2[u][j] * y2[u][j];
+#pragma unroll
+          for (int m = 1; m < TPH; m *= 2) ss += __shfl_xor(ss, m, 64);
+          const float rs = 1.0f / sqrtf(ss / (float)HD + a.eps);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            y1[u][j] = y1[u][j] * rs * (is_q ? gq1[j] : gk1[j]);
+            y2[u][j] = y2[u][j] * rs * (is_q ? gq2[j] : gk2[j]);
+          }
+        }
+        if (a.rotate) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float e = y1[u][j], f = y2[u][j];
+            y1[u][j] = e * cs[j] - f * sn[j];
+            y2[u][j] = f * cs[j] + e * sn[j];
+          }
+        }
+        if (is_q) {
+          const size_t o = (size_t)(row_lo + r) * a.ldqo + (size_t)hh * HD + d;
+          store8<IO>(a.q_out, o, y1[u]);
+          store8<IO>(a.q_out, o + HALF, y2[u]);
+        } else {
+          const size_t base = (size_t)(b * a.n_kv + hh) * a.kv_len * HD;
+          if constexpr (DT == RV_BF16) {
+            store_pair8(a.kc, a.kc2, base + k_elem(p, d, HD), y1[u]);
+            store_pair8(a.kc, a.kc2, base + k_elem(p, HALF + d, HD), y2[u]);
+          } else {
+            store8<RV_F32>(a.kc, base + (size_t)p * HD + d, y1[u]);
+            store8<RV_F32>(a.kc, base + (size_t)p * HD + HALF + d, y2[u]);
+          }
+        }
       }
     }
-    if (is_q) {
-      const size_t o = (size_t)(row_lo + r) * a.ldqo + (size_t)hh * HD + d;
-      store8<IO>(a.q_out, o, y1);
-      store8<IO>(a.q_out, o + HALF, y2);
-    } else {
-      const size_t base = (size_t)(b * a.n_kv + hh) * a.kv_len * HD;
-      if constexpr (DT == RV_BF16) {
-        store_pair8(a.kc, a.kc2, base + k_elem(p, d, HD), y1);
-        store_pair8(a.kc, a.kc2, base + k_elem(p, HALF + d, HD), y2);
-      } else {
-        store8<RV_F32>(a.kc, base + (size_t)p * HD + d, y1);
-        store8<RV_F32>(a.kc, base + (size_t)p * HD + HALF + d, y2);
-      }
-    }
+    return;
   }
 
-  // v heads
-  for (int h = max(h_lo, n_qk); h < h_end; ++h) {
-    const int hh = h - n_qk;
-    const size_t base = (size_t)(b * a.n_kv + hh) * a.kv_len * HD;
-    __syncthreads();  // the last head's rows have been read
-    for (int i = tid; i < rows * (HD / 8); i += 256) {
-      const int r = i / (HD / 8), d = i % (HD / 8) * 8;
-      float y[8];
-      load8<IO>(a.v, (size_t)(row_lo + r) * a.ldv + (size_t)hh * HD + d, y);
-      if constexpr (DT == RV_F32) {
-        store8<RV_F32>(a.vc, base + (size_t)(p_lo + r) * HD + d, y);
-      } else {
-        const int kk = p_lo + r - blk * kBlockPos;
+  // one v head
+  const int hh = blockIdx.y - a.qk_groups;
+  const size_t base = (size_t)(b * a.n_kv + hh) * a.kv_len * HD;
+  for (int i = tid; i < rows * (HD / 8); i += 256) {
+    const int r = i / (HD / 8), d = i % (HD / 8) * 8;
+    float y[8];
+    load8<IO>(a.v, (size_t)(row_lo + r) * a.ldv + (size_t)hh * HD + d, y);
+    if constexpr (DT == RV_F32) {
+      store8<RV_F32>(a.vc, base + (size_t)(p_lo + r) * HD + d, y);
+    } else {
+      const int kk = p_lo + r - blk * kBlockPos;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sv[kk][d + j] = y[j];
-      }
+      for (int j = 0; j < 8; ++j) sv[kk][d + j] = y[j];
     }
-    if constexpr (DT == RV_BF16) {
-      __syncthreads();
-      const int k_lo = p_lo - blk * kBlockPos, k_hi = p_hi - blk * kBlockPos;
-      for (int i = tid; i < HD * 4; i += 256) {
-        const int g = i / HD, d = i % HD;  // keys 4g..4g+3 and 16+4g..16+4g+3 of the block
-        const size_t at = base + v_elem(blk * kBlockPos + 4 * g, d, HD);
-        float y[8];
-        bool all = true;
+  }
+  if constexpr (DT == RV_BF16) {
+    __syncthreads();
+    const int k_lo = p_lo - blk * kBlockPos, k_hi = p_hi - blk * kBlockPos;
+    for (int i = tid; i < HD * 4; i += 256) {
+      const int g = i / HD, d = i % HD;  // keys 4g..4g+3 and 16+4g..16+4g+3 of the block
+      if (!group_touched(g, k_lo, k_hi)) continue;
+      const size_t at = base + v_elem(blk * kBlockPos + 4 * g, d, HD);
+      float y[8];
+      bool all = true;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int kk = 4 * g + (j & 3) + 16 * (j >> 2);
+        all = all && kk >= k_lo && kk < k_hi;
+        y[j] = sv[kk][d];
+      }
+      if (all) {
+        store_pair8(a.vc, a.vc2, at, y);
+      } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int kk = 4 * g + (j & 3) + 16 * (j >> 2);
-          all = all && kk >= k_lo && kk < k_hi;
-          y[j] = sv[kk][d];
-        }
-        if (all) {
-          store_pair8(a.vc, a.vc2, at, y);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int kk = 4 * g + (j & 3) + 16 * (j >> 2);
-            if (kk < k_lo || kk >= k_hi) continue;
-            const uint16_t hb = f2bf(y[j]);
-            ((uint16_t*)a.vc)[at + j] = hb;
-            ((uint16_t*)a.vc2)[at + j] = f2bf(y[j] - bf2f(hb));
-          }
+          if (kk < k_lo || kk >= k_hi) continue;
+          const uint16_t hb = f2bf(y[j]);
+          ((uint16_t*)a.vc)[at + j] = hb;
+          ((uint16_t*)a.vc2)[at + j] = f2bf(y[j] - bf2f(hb));
         }
       }
     }
@@ -229,8 +258,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
       __syncthreads();  // the last head's rows have been read
       for (int i = tid; i < HD * 4; i += 256) {
         const int g = i / HD, d = i % HD;
-        // groups without a row of the call are left out
-        if (!(4 * g < k_hi && 4 * g + 4 > k_lo) && !(16 + 4 * g < k_hi && 20 + 4 * g > k_lo)) continue;
+        if (!group_touched(g, k_lo, k_hi)) continue;
         float y[8];
         load_pair8(a.vc, a.vc2, base + v_elem(blk * kBlockPos + 4 * g, d, HD), y);
 #pragma unroll
@@ -275,7 +303,7 @@ RV_DEV void run_moves(const CopyProgram& p, int unit, Addr addr, On on, int step
       const V* s = addr(p.src[m]);
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (i * step < left) v[u][i] = p.from_saved[m] ? saved[i] : s[i * step];
+        if (i * step < left) v[u][i] = p.from_saved[m] ? saved[i] : __builtin_nontemporal_load(s + i * step);
     }
 #pragma unroll
     for (int u = 0; u < kMoveBatch; ++u) {
@@ -284,7 +312,7 @@ RV_DEV void run_moves(const CopyProgram& p, int unit, Addr addr, On on, int step
       V* d = addr(p.dst[m]);
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        if (i * step < left) d[i * step] = v[u][i];
+        if (i * step < left) __builtin_nontemporal_store(v[u][i], d + i * step);
     }
   }
 }
@@ -360,9 +388,13 @@ int heads_per_wg(int max_rows, int threads_per_row, int heads) {
 int span_blocks(int pos, int rows) { return rows ? (pos + rows - 1) / kBlockPos - pos / kBlockPos + 1 : 0; }
 
 hipError_t launch_append(int dtype, int io, int hd, int max_rows, AppendArgs& a, hipStream_t st) {
-  const int heads = a.n_heads + 2 * a.n_kv;
-  a.hpw = heads_per_wg(max_rows, hd / 16, heads);
-  const dim3 grid(a.blk0[a.B], (heads + a.hpw - 1) / a.hpw);
+  // heads side by side, and as many rounds of them as leave four workgroups to a CU
+  const int heads = a.n_heads + a.n_kv, par = heads_per_wg(max_rows, hd / 16, heads);
+  int rounds = kHeadBatch;
+  while (rounds > 1 && (long long)a.blk0[a.B] * ((heads + par * rounds - 1) / (par * rounds)) < 1024) rounds /= 2;
+  a.hpw = par * rounds;
+  a.qk_groups = (heads + a.hpw - 1) / a.hpw;
+  const dim3 grid(a.blk0[a.B], a.qk_groups + a.n_kv);
   if (dtype == RV_BF16)
     return io == RV_F32 ? append_hd<RV_BF16, RV_F32>(a, hd, grid, st) : append_hd<RV_BF16, RV_BF16>(a, hd, grid, st);
   return io == RV_F32 ? append_hd<RV_F32, RV_F32>(a, hd, grid, st) : append_hd<RV_F32, RV_BF16>(a, hd, grid, st);

@@ -150,8 +150,11 @@ RV_DEV size_t part_index(const ShareArgs& a, int slot, int row, int head) {
 
 // Softmax weights of one query's scores of NB 16-key blocks: masks keys past
 // the limit, folds them into (m, l) and leaves 2^(s - m) in s.  Returns the
-// factor for what was summed before.  A wave whose queries all see nothing yet
-// keeps m = -inf, weights 0.
+// factor for what was summed before.  m follows the largest score only where one
+// exceeds it by more than kSlack, for the whole wave at once, so that most tiles
+// rescale nothing; weights then stay below 2^kSlack.  A wave whose queries all
+// see nothing yet keeps m = -inf, weights 0.
+constexpr float kSlack = 6.0f;
 template <int NB>
 RV_DEV float softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, float sc, bool masked, float& m, float& l) {
   float top = -INFINITY;
@@ -165,20 +168,23 @@ RV_DEV float softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, f
       }
       top = fmaxf(top, s[t][i]);
     }
-  top = rows4_max(top);
-  const float m_new = fmaxf(m, top * sc);
-  const float m_use = m_new == -INFINITY ? 0.f : m_new;
-  const float rescale = __builtin_amdgcn_exp2f(m - m_use);
+  top = rows4_max(top) * sc;
+  float rescale = 1.0f;
+  if (__any(top > m + kSlack)) {
+    const float m_new = fmaxf(m, top);
+    rescale = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+  }
+  const float base = m == -INFINITY ? 0.f : m;
   float sum = 0.f;
 #pragma unroll
   for (int t = 0; t < NB; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], sc, -m_use));
+      s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], sc, -base));
       sum += s[t][i];
     }
   l = l * rescale + rows4_sum(sum);
-  m = m_new;
   return rescale;
 }
 
@@ -202,57 +208,62 @@ RV_DEV f32x4_t mfma(const u32x4& x, const bf16x8_t& y, const f32x4_t& acc) {
 // the queries that see them get NaN instead (what the pair (inf, inf - inf)
 // stands for).  v: V operands of a 32-key chunk, vis: per key slot whether the
 // lane's query sees it.
-RV_DEV bool not_finite_bf16x2(uint32_t x) {
-  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-}
+// Bits 15 and 31: the two bf16 of x that are not finite (exponent all ones).
+RV_DEV uint32_t not_finite2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 template <int DT>
 RV_DEV bool any_not_finite(const u32x4 (&vh)[DT]) {
-  bool bad = false;
+  uint32_t bad = 0;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) bad |= not_finite_bf16x2(vh[d][j]);
-  return __any(bad);
+    for (int j = 0; j < 4; ++j) bad |= not_finite2(vh[d][j]);
+  return __any(bad != 0);
 }
-template <int DT>
-RV_DEV void take_out(u32x4 (&vh)[DT], u32x4 (&vl)[DT], int k0, int kend, int last, int g, f32x4_t (&O)[DT]) {
-  bf16x8_t vis;
+// O[t][d0 + d] is query tile t's; last[t] the last key its query sees.
+template <int ND, int TPW, int DT>
+RV_DEV void take_out(u32x4 (&vh)[ND], u32x4 (&vl)[ND], int k0, int kend, const Query (&q)[TPW], int g,
+                     f32x4_t (&O)[TPW][DT], int d0) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int key = k0 + 4 * g + (j & 3) + 16 * (j >> 2);
-    vis[j] = (__bf16)(key < kend && key <= last ? 1.0f : 0.0f);
-  }
-#pragma unroll
-  for (int d = 0; d < DT; ++d) {
+  for (int d = 0; d < ND; ++d) {
     u32x4 mark;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      uint32_t keep = 0, ones = 0;
-      if ((vh[d][j] & 0x7f80u) != 0x7f80u) keep |= 0xffffu;
-      else ones |= 0x3f80u;
-      if ((vh[d][j] & 0x7f800000u) != 0x7f800000u) keep |= 0xffff0000u;
-      else ones |= 0x3f800000u;
+      const uint32_t bad = not_finite2(vh[d][j]) >> 15;  // 0 or 1 in each half
+      const uint32_t keep = ~(bad * 0xffffu);
+      mark[j] = bad * 0x3f80u;  // 1.0
       vh[d][j] &= keep;
       vl[d][j] &= keep;
-      mark[j] = ones;
     }
-    const f32x4_t seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, mark), vis,
-                                                                 f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (seen[i] > 0.f) O[d][i] = __builtin_nanf("");
+    for (int t = 0; t < TPW; ++t) {
+      bf16x8_t vis;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = k0 + 4 * g + (j & 3) + 16 * (j >> 2);
+        vis[j] = (__bf16)(key < kend && key <= q[t].last ? 1.0f : 0.0f);
+      }
+      const f32x4_t seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, mark), vis,
+                                                                   f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (seen[i] > 0.f) O[t][d0 + d][i] = __builtin_nanf("");
+    }
   }
 }
 
 // ----------------------------------------------------------- bf16, many queries
 // S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMAs, operands as pairs of planes
-// (three products each, lo lo dropped: 2^-16 of the result), 8 waves of one
-// 16-query tile.  The cache holds tiles in operand order (k_elem / v_elem): a
-// 64-key tile is four spans that go global -> LDS directly, double-buffered.
-template <int HD, int PART>
+// (three products each, lo lo dropped: 2^-16 of the result; queries given in
+// bf16 have no lo plane, two products).  8 waves of TPW 16-query tiles: every
+// K and V operand read from LDS serves TPW tiles, and with one LDS reads bound
+// the kernel (512 KiB a tile and CU against 3072 cycles of MFMA), so calls with
+// more than 128 queries take two.  The cache holds tiles in operand order (k_elem
+// / v_elem): a 64-key tile is four spans that go global -> LDS directly,
+// double-buffered.
+template <int HD, int PART, int TPW, bool QLO>
 __global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
   constexpr int NW = 8, DC = HD / 32, DT = HD / 16, SPAN = kKB * HD;
-  constexpr int UPW = 4 * SPAN / 512 / NW;  // 1 KiB pieces each wave copies
+  constexpr int UPW = 4 * SPAN / 512 / NW;  // 1 KiB pieces each wave copies, all of one span
   __shared__ __attribute__((aligned(16))) uint16_t sm0[4][SPAN];
   __shared__ __attribute__((aligned(16))) uint16_t sm1[4][SPAN];
   Unit u;
@@ -260,72 +271,107 @@ __global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
 
+  const int sp = w / 2, off = (w & 1) * (SPAN / 2);
+  const uint16_t* plane = (const uint16_t*)(sp == 0 ? a.kc : sp == 1 ? a.kc2 : sp == 2 ? a.vc : a.vc2) + off;
   auto fetch = [&](uint16_t(&sm)[4][SPAN], int k0) {
-    const size_t at = tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + lane * 8;
+    const uint16_t* src = plane + tile_base<HD>(a, u.seq, u.kvh, k0 / kKB);
+    auto* dst = (__attribute__((address_space(3))) char*)(&sm[0][0] + sp * SPAN + off);
 #pragma unroll
-    for (int i = 0; i < UPW; ++i) {
-      const int piece = w * UPW + i, sp = piece / (SPAN / 512), off = piece % (SPAN / 512) * 512;
-      const void* base = sp == 0 ? a.kc : sp == 1 ? a.kc2 : sp == 2 ? a.vc : a.vc2;
-      __builtin_amdgcn_global_load_lds((const void*)((const uint16_t*)base + at + off),
-                                       (__attribute__((address_space(3))) void*)(&sm[0][0] + sp * SPAN + off), 16, 0, 0);
-    }
+    for (int i = 0; i < UPW; ++i)
+      __builtin_amdgcn_global_load_lds((const void*)(src + lane * 8 + i * 512),
+                                       (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
   };
   fetch(sm0, u.kbeg);
 
-  const bool active = u.q_begin + 16 * w < u.nq;
-  const Query q = query_of<PART>(a, u, u.q_begin + 16 * w + (lane & 15));
+  const int q0 = u.q_begin + 16 * TPW * w;
+  const bool active = q0 < u.nq;
   const int first_last = first_limit<PART>(a, u);
-  u32x4 qh[DC], ql[DC];
-  load_query<HD>(a, q, g, qh, ql);
-  float m = -INFINITY, l = 0.f;
-  f32x4_t O[DT];
+  Query q[TPW];
+  u32x4 qh[TPW][DC], ql[TPW][DC];
 #pragma unroll
-  for (int d = 0; d < DT; ++d) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < TPW; ++t) {
+    q[t] = query_of<PART>(a, u, q0 + 16 * t + (lane & 15));
+    load_query<HD>(a, q[t], g, qh[t], ql[t]);
+  }
+  float m[TPW], l[TPW];
+  f32x4_t O[TPW][DT];
+#pragma unroll
+  for (int t = 0; t < TPW; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) O[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
 
   auto tile = [&](const uint16_t(&sm)[4][SPAN], int k0) {
     if (!active) return;
-    f32x4_t s[4];
+    f32x4_t s[TPW][4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < TPW; ++t)
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) s[t][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < DC; ++c) {
-      const bf16x8_t h = __builtin_bit_cast(bf16x8_t, qh[c]), lo = __builtin_bit_cast(bf16x8_t, ql[c]);
       u32x4 kh[4], kl[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        kh[t] = *(const u32x4*)(&sm[0][(t * DC + c) * 512 + lane * 8]);
-        kl[t] = *(const u32x4*)(&sm[1][(t * DC + c) * 512 + lane * 8]);
+      for (int kb = 0; kb < 4; ++kb) {
+        kh[kb] = *(const u32x4*)(&sm[0][(kb * DC + c) * 512 + lane * 8]);
+        kl[kb] = *(const u32x4*)(&sm[1][(kb * DC + c) * 512 + lane * 8]);
       }
 #pragma unroll
-      for (int t = 0; t < 4; ++t) s[t] = mfma(kh[t], h, s[t]);
+      for (int t = 0; t < TPW; ++t)
 #pragma unroll
-      for (int t = 0; t < 4; ++t) s[t] = mfma(kh[t], lo, s[t]);
+        for (int kb = 0; kb < 4; ++kb) s[t][kb] = mfma(kh[kb], __builtin_bit_cast(bf16x8_t, qh[t][c]), s[t][kb]);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) s[t] = mfma(kl[t], h, s[t]);
+      for (int t = 0; t < TPW; ++t)
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) s[t][kb] = mfma(kl[kb], __builtin_bit_cast(bf16x8_t, qh[t][c]), s[t][kb]);
+      if constexpr (QLO) {
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int kb = 0; kb < 4; ++kb) s[t][kb] = mfma(kh[kb], __builtin_bit_cast(bf16x8_t, ql[t][c]), s[t][kb]);
+      }
     }
-    const bool masked = k0 + kKB > u.kend || k0 + kKB - 1 > first_last;
-    const float rescale = softmax_step<4>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l);
-    if (__any(rescale != 1.0f)) {
+    const bool masked = PART && (k0 + kKB > u.kend || k0 + kKB - 1 > first_last);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] *= rescale;
+    for (int t = 0; t < TPW; ++t) {
+      const float rescale = softmax_step<4>(s[t], k0, u.kend, q[t].last, g, a.scale_log2, masked, m[t], l[t]);
+      if (__any(rescale != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[t][d] *= rescale;
+      }
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      bf16x8_t ph, pl;
-      split_p(s[2 * c], s[2 * c + 1], ph, pl);
-      u32x4 vh[DT], vl[DT];
+      bf16x8_t ph[TPW], pl[TPW];
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        vh[d] = *(const u32x4*)(&sm[2][(c * DT + d) * 512 + lane * 8]);
-        vl[d] = *(const u32x4*)(&sm[3][(c * DT + d) * 512 + lane * 8]);
+      for (int t = 0; t < TPW; ++t) split_p(s[t][2 * c], s[t][2 * c + 1], ph[t], pl[t]);
+      // four d tiles at a time: their operands, then the products in passes, so
+      // that dependent MFMAs are 4 TPW apart
+#pragma unroll
+      for (int d0 = 0; d0 < DT; d0 += DT < 4 ? DT : 4) {
+        constexpr int ND = DT < 4 ? DT : 4;
+        u32x4 vh[ND], vl[ND];
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          vh[d] = *(const u32x4*)(&sm[2][(c * DT + d0 + d) * 512 + lane * 8]);
+          vl[d] = *(const u32x4*)(&sm[3][(c * DT + d0 + d) * 512 + lane * 8]);
+        }
+        if (masked && any_not_finite<ND>(vh)) take_out<ND, TPW, DT>(vh, vl, k0 + 32 * c, u.kend, q, g, O, d0);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) O[t][d0 + d] = mfma(vh[d], ph[t], O[t][d0 + d]);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) O[t][d0 + d] = mfma(vh[d], pl[t], O[t][d0 + d]);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int d = 0; d < ND; ++d) O[t][d0 + d] = mfma(vl[d], ph[t], O[t][d0 + d]);
       }
-      if (masked && any_not_finite<DT>(vh)) take_out<DT>(vh, vl, k0 + 32 * c, u.kend, q.last, g, O);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] = mfma(vh[d], ph, O[d]);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] = mfma(vh[d], pl, O[d]);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] = mfma(vl[d], ph, O[d]);
     }
   };
 
@@ -345,19 +391,22 @@ __global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
   }
 
   // lane holds O^T[d = 16t + 4g + i][query lane%16]
-  if (!q.valid) return;
-  if (a.direct) {
-    const float inv = 1.0f / l;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) put_out4<RV_BF16>(a, HD, q.row, q.head, 16 * d + 4 * g, O[d] * inv);
-    return;
-  }
-  const size_t e = part_index(a, u.slot, q.row, q.head);
+  for (int t = 0; t < TPW; ++t) {
+    if (!q[t].valid) continue;
+    if (a.direct) {
+      const float inv = 1.0f / l[t];
 #pragma unroll
-  for (int d = 0; d < DT; ++d) *(f32x4_t*)(a.part_o + e * HD + 16 * d + 4 * g) = O[d];
-  if (g == 0) {
-    a.part_ml[2 * e] = m;
-    a.part_ml[2 * e + 1] = l;
+      for (int d = 0; d < DT; ++d) put_out4<RV_BF16>(a, HD, q[t].row, q[t].head, 16 * d + 4 * g, O[t][d] * inv);
+      continue;
+    }
+    const size_t e = part_index(a, u.slot, q[t].row, q[t].head);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *(f32x4_t*)(a.part_o + e * HD + 16 * d + 4 * g) = O[t][d];
+    if (g == 0) {
+      a.part_ml[2 * e] = m[t];
+      a.part_ml[2 * e + 1] = l[t];
+    }
   }
 }
 
@@ -404,14 +453,14 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
     load_v(next);
   }
   next = at(min(k0 + NW * KT, last_tile));
-  const Query q = query_of<PART>(a, u, u.q_begin + (lane & 15));
+  const Query q[1] = {query_of<PART>(a, u, u.q_begin + (lane & 15))};
   const int first_last = first_limit<PART>(a, u);
   u32x4 qh[DC], ql[DC];
-  load_query<HD>(a, q, g, qh, ql);
+  load_query<HD>(a, q[0], g, qh, ql);
   float m = -INFINITY, l = 0.f;
-  f32x4_t O[DT];
+  f32x4_t O[1][DT];
 #pragma unroll
-  for (int d = 0; d < DT; ++d) O[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int d = 0; d < DT; ++d) O[0][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   for (; k0 < u.kend; k0 += NW * KT) {
     f32x4_t s[NB];
@@ -429,20 +478,21 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
     }
     load_k(next);
     const bool masked = k0 + KT > u.kend || k0 + KT - 1 > first_last;
-    const float rescale = softmax_step<NB>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l);
+    const float rescale = softmax_step<NB>(s, k0, u.kend, q[0].last, g, a.scale_log2, masked, m, l);
 #pragma unroll
-    for (int d = 0; d < DT; ++d) O[d] *= rescale;
+    for (int d = 0; d < DT; ++d) O[0][d] *= rescale;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       bf16x8_t ph, pl;
       split_p(s[2 * c], s[2 * c + 1], ph, pl);
-      if (masked && any_not_finite<DT>(v[0][c])) take_out<DT>(v[0][c], v[1][c], k0 + 32 * c, u.kend, q.last, g, O);
+      if (masked && any_not_finite<DT>(v[0][c])) 
+        take_out<DT, 1, DT>(v[0][c], v[1][c], k0 + 32 * c, u.kend, q, g, O, 0);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] = mfma(v[0][c][d], ph, O[d]);
+      for (int d = 0; d < DT; ++d) O[0][d] = mfma(v[0][c][d], ph, O[0][d]);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] = mfma(v[0][c][d], pl, O[d]);
+      for (int d = 0; d < DT; ++d) O[0][d] = mfma(v[0][c][d], pl, O[0][d]);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] = mfma(v[1][c][d], ph, O[d]);
+      for (int d = 0; d < DT; ++d) O[0][d] = mfma(v[1][c][d], ph, O[0][d]);
     }
     load_v(next);
     next = at(min(k0 + 2 * NW * KT, last_tile));
@@ -450,7 +500,7 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
 
   // merge the waves: one without tiles has m = -inf, l = 0, O = 0
 #pragma unroll
-  for (int d = 0; d < DT; ++d) *(f32x4_t*)&red_o[w][lane & 15][16 * d + 4 * g] = O[d];
+  for (int d = 0; d < DT; ++d) *(f32x4_t*)&red_o[w][lane & 15][16 * d + 4 * g] = O[0][d];
   if (g == 0) {
     red_m[w][lane & 15] = m;
     red_l[w][lane & 15] = l;
@@ -655,7 +705,10 @@ hipError_t launch_part(int dtype, const ShareArgs& a, hipStream_t st) {
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
   if (dtype == RV_F32) k_share_f32<HD, PART><<<(unsigned)grid, 64, 0, st>>>(a);
   else if (sp.qpw == 16) k_share_few<HD, PART><<<(unsigned)grid, 512, 0, st>>>(a);
-  else k_share_many<HD, PART><<<(unsigned)grid, 512, 0, st>>>(a);
+  else if (sp.qpw == 128 && a.q_kind == RV_BF16) k_share_many<HD, PART, 1, false><<<(unsigned)grid, 512, 0, st>>>(a);
+  else if (sp.qpw == 128) k_share_many<HD, PART, 1, true><<<(unsigned)grid, 512, 0, st>>>(a);
+  else if (a.q_kind == RV_BF16) k_share_many<HD, PART, 2, false><<<(unsigned)grid, 512, 0, st>>>(a);
+  else k_share_many<HD, PART, 2, true><<<(unsigned)grid, 512, 0, st>>>(a);
   return hipGetLastError();
 }
 

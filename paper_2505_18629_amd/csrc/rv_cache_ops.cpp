@@ -6,10 +6,11 @@
 
 namespace {
 
-// The row spans of a call: sequence b has h_rows[b] rows at positions h_pos[b] ..
-// Fills pos, row0 and (blk0 not NULL) blk0; *max_rows the longest span.
-rv_status check_spans(const rv_cache* c, const int32_t* h_pos, const int32_t* h_rows, int* pos, int* row0, int* blk0,
-                      int* max_rows) {
+// The row spans of a call: sequence b has h_rows[b] rows at positions h_pos[b] ..,
+// n_rows together.  Fills pos, row0 and (blk0 not NULL) blk0; *max_rows the longest span.
+rv_status check_spans(const rv_cache* c, int32_t batch, const int32_t* h_pos, const int32_t* h_rows, int64_t n_rows,
+                      int* pos, int* row0, int* blk0, int* max_rows) {
+  if (batch != c->B) return rv_fail(RV_E_ARG, "positions and counts of %d sequences, the cache has %d", batch, c->B);
   long long rows = 0, blocks = 0;
   *max_rows = 0;
   for (int b = 0; b < c->B; ++b) {
@@ -27,6 +28,7 @@ rv_status check_spans(const rv_cache* c, const int32_t* h_pos, const int32_t* h_
   }
   row0[c->B] = (int)rows;
   if (blk0) blk0[c->B] = (int)blocks;
+  if (rows != n_rows) return rv_fail(RV_E_ARG, "counts add up to %lld rows, given are %lld", rows, (long long)n_rows);
   return RV_OK;
 }
 
@@ -37,10 +39,11 @@ rv_status check_layer(const rv_cache* c, int32_t layer) {
 }
 
 // Rows that the kernels read and write 16 bytes at a time.
-rv_status check_rows(const char* what, const void* d, int64_t ld, int width, int io) {
+rv_status check_rows(const char* what, const void* d, int64_t ld, int64_t width, int want, int io) {
+  if (width != want) return rv_fail(RV_E_ARG, "%s: rows of %lld values, the model's have %d", what, (long long)width, want);
   if (!d) return rv_fail(RV_E_ARG, "%s rows are NULL", what);
   const int per16 = io == RV_F32 ? 4 : 8;
-  if (ld < width) return rv_fail(RV_E_ARG, "%s: row stride %lld below the width %d", what, (long long)ld, width);
+  if (ld < width) return rv_fail(RV_E_ARG, "%s: row stride %lld below the width %d", what, (long long)ld, want);
   if (((uintptr_t)d & 15) || ld % per16)
     return rv_fail(RV_E_ARG, "%s: rows must start at multiples of 16 bytes", what);
   return RV_OK;
@@ -150,7 +153,7 @@ rv_status rv_cache_dims(const rv_cache* c, int32_t* h_dims) {
   return RV_OK;
 }
 
-rv_status rv_cache_append(rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows,
+rv_status rv_cache_append(rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
                           const rv_rows* rows, void* stream) {
   if (!c || !h_pos || !h_rows || !rows) return rv_fail(RV_E_ARG, "cache, positions, counts and rows must not be NULL");
   if (rv_status s = check_layer(c, layer); s != RV_OK) return s;
@@ -159,16 +162,17 @@ rv_status rv_cache_append(rv_cache* c, int32_t layer, const int32_t* h_pos, cons
   if (io != RV_F32 && io != RV_BF16) return rv_fail(RV_E_ARG, "rows must be RV_F32 or RV_BF16");
   AppendArgs a{};
   int max_rows = 0;
-  if (rv_status s = check_spans(c, h_pos, h_rows, a.pos, a.row0, a.blk0, &max_rows); s != RV_OK) return s;
+  if (rv_status s = check_spans(c, batch, h_pos, h_rows, rows->n_rows, a.pos, a.row0, a.blk0, &max_rows); s != RV_OK)
+    return s;
   for (int b = 0; b < c->B; ++b)
     if (rv_status s = check_writable(c, b, h_pos[b], h_rows[b]); s != RV_OK) return s;
   if (!max_rows) return RV_OK;
-  if (rv_status s = check_rows("k", rows->d_k, rows->ld_k, kvd, io); s != RV_OK) return s;
-  if (rv_status s = check_rows("v", rows->d_v, rows->ld_v, kvd, io); s != RV_OK) return s;
+  if (rv_status s = check_rows("k", rows->d_k, rows->ld_k, rows->kv_width, kvd, io); s != RV_OK) return s;
+  if (rv_status s = check_rows("v", rows->d_v, rows->ld_v, rows->kv_width, kvd, io); s != RV_OK) return s;
   if (!rows->d_q != !rows->d_q_out) return rv_fail(RV_E_ARG, "q and its output come together");
   if (rows->d_q) {
-    if (rv_status s = check_rows("q", rows->d_q, rows->ld_q, qd, io); s != RV_OK) return s;
-    if (rv_status s = check_rows("q output", rows->d_q_out, rows->ld_q_out, qd, io); s != RV_OK) return s;
+    if (rv_status s = check_rows("q", rows->d_q, rows->ld_q, rows->q_width, qd, io); s != RV_OK) return s;
+    if (rv_status s = check_rows("q output", rows->d_q_out, rows->ld_q_out, rows->q_width, qd, io); s != RV_OK) return s;
   }
   const Planes p = layer_planes(c, layer);
   a.q = rows->d_q;
@@ -197,19 +201,21 @@ rv_status rv_cache_append(rv_cache* c, int32_t layer, const int32_t* h_pos, cons
   return RV_OK;
 }
 
-rv_status rv_cache_read(const rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows, int32_t dtype,
-                        void* d_k, int64_t ld_k, void* d_v, int64_t ld_v, void* stream) {
+rv_status rv_cache_read(const rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
+                        int32_t dtype, int64_t n_rows, int64_t width, void* d_k, int64_t ld_k, void* d_v, int64_t ld_v,
+                        void* stream) {
   if (!c || !h_pos || !h_rows) return rv_fail(RV_E_ARG, "cache, positions and counts must not be NULL");
   if (rv_status s = check_layer(c, layer); s != RV_OK) return s;
   const rv_config& mc = c->m->cfg;
   if (dtype != RV_F32 && dtype != RV_BF16) return rv_fail(RV_E_ARG, "rows must be RV_F32 or RV_BF16");
   ReadArgs a{};
   int max_rows = 0;
-  if (rv_status s = check_spans(c, h_pos, h_rows, a.pos, a.row0, a.blk0, &max_rows); s != RV_OK) return s;
+  if (rv_status s = check_spans(c, batch, h_pos, h_rows, n_rows, a.pos, a.row0, a.blk0, &max_rows); s != RV_OK)
+    return s;
   if (!max_rows) return RV_OK;
   const int kvd = mc.n_kv_heads * mc.head_dim;
-  if (rv_status s = check_rows("k", d_k, ld_k, kvd, dtype); s != RV_OK) return s;
-  if (rv_status s = check_rows("v", d_v, ld_v, kvd, dtype); s != RV_OK) return s;
+  if (rv_status s = check_rows("k", d_k, ld_k, width, kvd, dtype); s != RV_OK) return s;
+  if (rv_status s = check_rows("v", d_v, ld_v, width, kvd, dtype); s != RV_OK) return s;
   const Planes p = layer_planes(c, layer);
   a.k = d_k;
   a.v = d_v;
@@ -337,20 +343,22 @@ rv_status rv_cache_fork(rv_cache* c, int32_t src, int32_t len, int32_t n, const 
   return RV_OK;
 }
 
-rv_status rv_cache_attend(const rv_cache* c, int32_t layer, const int32_t* h_pos, const int32_t* h_rows, int32_t dtype,
-                          const void* d_q, int64_t ld_q, void* d_out, int64_t ld_out, void* stream) {
+rv_status rv_cache_attend(const rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
+                          int32_t dtype, int64_t n_rows, int64_t width, const void* d_q, int64_t ld_q, void* d_out,
+                          int64_t ld_out, void* stream) {
   if (!c || !h_pos || !h_rows) return rv_fail(RV_E_ARG, "cache, positions and counts must not be NULL");
   if (rv_status s = check_layer(c, layer); s != RV_OK) return s;
   const rv_config& mc = c->m->cfg;
   if (dtype != RV_F32 && dtype != RV_BF16) return rv_fail(RV_E_ARG, "rows must be RV_F32 or RV_BF16");
   int pos[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1], max_rows = 0;
-  if (rv_status s = check_spans(c, h_pos, h_rows, pos, row0, nullptr, &max_rows); s != RV_OK) return s;
+  if (rv_status s = check_spans(c, batch, h_pos, h_rows, n_rows, pos, row0, nullptr, &max_rows); s != RV_OK)
+    return s;
   if (!max_rows) return RV_OK;
   if (row0[c->B] > c->rows_cap)
     return rv_fail(RV_E_CAPACITY, "%d rows, the cache's workspace holds %d", row0[c->B], c->rows_cap);
   const int qd = mc.n_heads * mc.head_dim;
-  if (rv_status s = check_rows("q", d_q, ld_q, qd, dtype); s != RV_OK) return s;
-  if (rv_status s = check_rows("output", d_out, ld_out, qd, dtype); s != RV_OK) return s;
+  if (rv_status s = check_rows("q", d_q, ld_q, width, qd, dtype); s != RV_OK) return s;
+  if (rv_status s = check_rows("output", d_out, ld_out, width, qd, dtype); s != RV_OK) return s;
   ShareArgs a{};
   plan_attend(c, pos, row0, a);
   const Planes p = layer_planes(c, layer);

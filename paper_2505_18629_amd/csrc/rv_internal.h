@@ -252,7 +252,8 @@ struct AppendArgs {
   bool rotate;
   const float *rope_cos, *rope_sin;
   void *kc, *vc, *kc2, *vc2;  // this layer's cache planes
-  int n_heads, n_kv, kv_len, B, hpw;  // n_heads 0: no q; hpw is the launcher's
+  int n_heads, n_kv, kv_len, B;  // n_heads 0: no q
+  int hpw, qk_groups;            // the launcher's
   int pos[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1], blk0[RV_MAX_BATCH + 1];
 };
 struct ReadArgs {

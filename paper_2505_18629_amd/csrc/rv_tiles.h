@@ -288,7 +288,7 @@ inline SharePart plan_part(bool bf16, const ShareUnit* u, int n, int n_kv, int h
     qmax = std::max(qmax, u[i].queries);
   }
   if (!kmax || !qmax) return s;
-  s.qpw = !bf16 || qmax <= 16 ? 16 : 128;
+  s.qpw = !bf16 || qmax <= 16 ? 16 : qmax <= 128 ? 128 : 256;
   s.nqg = (qmax + s.qpw - 1) / s.qpw;
   static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80};
   double best = 0;
@@ -307,7 +307,7 @@ inline SharePart plan_part(bool bf16, const ShareUnit* u, int n, int n_kv, int h
       const double stream = (double)keys * n_kv * 8 * hd / 5.5e6;
       t = std::max((double)((wgs + 255) / 256) * std::min(ks, kmax) * 8 * hd / 4.5e4, stream);
     } else {
-      t = (double)((wgs + 255) / 256) * (ks / kTile + 2) * 2.9 * hd / 128;
+      t = (double)((wgs + 255) / 256) * (ks / kTile + 2) * (s.qpw == 128 ? 2.2 : 3.8) * hd / 128;
     }
     const int runs = (kmax + ks - 1) / ks;
     t += 0.05 * runs;

@@ -322,19 +322,19 @@ static void shares() {
   CHECK(grouped > 200);
 }
 
+alignas(16) static char mem[64];
 static void refusals() {
   Host h(4, 200);
   rv_cache* c = &h.c;
-  alignas(16) static char mem[64];
   int32_t pos[4] = {0, 0, 0, 0}, n[4] = {1, 0, 2, 0};
-  rv_rows ok{RV_F32, 1, mem, mem, mem, 128, 32, 32, mem, 128, nullptr, nullptr};
-  auto append = [&](rv_rows r, int layer = 0) { return rv_cache_append(c, layer, pos, n, &r, nullptr); };
+  rv_rows ok{RV_F32, 1, 3, 128, 32, mem, mem, mem, mem, 128, 32, 32, 128, nullptr, nullptr};
+  auto append = [&](rv_rows r, int layer = 0) { return rv_cache_append(c, layer, 4, pos, n, &r, nullptr); };
   CHECK(append(ok) == RV_OK && g_launches == 1);
   g_launches = 0;
   rv_rows r;
-  CHECK(rv_cache_append(nullptr, 0, pos, n, &ok, nullptr) == RV_E_ARG);
-  CHECK(rv_cache_append(c, 0, nullptr, n, &ok, nullptr) == RV_E_ARG);
-  CHECK(rv_cache_append(c, 0, pos, n, nullptr, nullptr) == RV_E_ARG);
+  CHECK(rv_cache_append(nullptr, 0, 4, pos, n, &ok, nullptr) == RV_E_ARG);
+  CHECK(rv_cache_append(c, 0, 4, nullptr, n, &ok, nullptr) == RV_E_ARG);
+  CHECK(rv_cache_append(c, 0, 4, pos, n, nullptr, nullptr) == RV_E_ARG);
   CHECK(append(ok, 1) == RV_E_ARG && append(ok, -1) == RV_E_ARG);
   CHECK((r = ok, r.dtype = 2, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.d_k = nullptr, append(r)) == RV_E_ARG);
@@ -344,11 +344,19 @@ static void refusals() {
   CHECK((r = ok, r.dtype = RV_BF16, r.ld_q = 132, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.d_q_out = nullptr, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.ld_q_out = 127, append(r)) == RV_E_ARG);
+  CHECK((r = ok, r.n_rows = 2, append(r)) == RV_E_ARG && (r = ok, r.q_width = 96, append(r)) == RV_E_ARG);
+  CHECK((r = ok, r.kv_width = 28, append(r)) == RV_E_ARG);
+  CHECK(rv_cache_append(c, 0, 3, pos, n, &ok, nullptr) == RV_E_ARG);
+  auto read = [&](int64_t rows, int io = RV_F32, void* v = mem, int w = 32, int batch = 4) {
+    return rv_cache_read(c, 0, batch, pos, n, io, rows, w, mem, 32, v, 32, nullptr);
+  };
+  auto attend = [&](int64_t rows, int io = RV_F32, void* o = mem, int w = 128, int64_t ld = 128, int batch = 4) {
+    return rv_cache_attend(c, 0, batch, pos, n, io, rows, w, mem, ld, o, 128, nullptr);
+  };
   auto spans = [&](int p2, int n2) {
     pos[2] = p2;
     n[2] = n2;
-    const rv_status a = append(ok), b = rv_cache_read(c, 0, pos, n, RV_F32, mem, 32, mem, 32, nullptr),
-                    d = rv_cache_attend(c, 0, pos, n, RV_F32, mem, 128, mem, 128, nullptr);
+    const rv_status a = (r = ok, r.n_rows = 1LL + n2, append(r)), b = read(1LL + n2), d = attend(1LL + n2);
     CHECK(a == b && b == d);
     pos[2] = 0;
     n[2] = 2;
@@ -358,16 +366,16 @@ static void refusals() {
   CHECK(spans(0x7fffffff, 0x7fffffff) == RV_E_RANGE && g_launches == 0);
   CHECK(spans(199, 1) == RV_OK && spans(-5, 0) == RV_OK);
   g_launches = 0;
-  CHECK(rv_cache_read(c, 0, pos, n, 7, mem, 32, mem, 32, nullptr) == RV_E_ARG);
-  CHECK(rv_cache_read(c, 0, pos, n, RV_F32, mem, 32, nullptr, 32, nullptr) == RV_E_ARG);
-  CHECK(rv_cache_attend(c, 0, pos, n, 7, mem, 128, mem, 128, nullptr) == RV_E_ARG);
-  CHECK(rv_cache_attend(c, 0, pos, n, RV_F32, mem, 64, mem, 128, nullptr) == RV_E_ARG);
-  CHECK(rv_cache_attend(c, 0, pos, n, RV_F32, mem, 128, nullptr, 128, nullptr) == RV_E_ARG);
+  CHECK(read(3, 7) == RV_E_ARG && read(3, RV_F32, nullptr) == RV_E_ARG && read(3, RV_F32, mem, 64) == RV_E_ARG);
+  CHECK(read(4) == RV_E_ARG && read(3, RV_F32, mem, 32, 5) == RV_E_ARG);
+  CHECK(attend(3, 7) == RV_E_ARG && attend(3, RV_F32, nullptr) == RV_E_ARG && attend(2) == RV_E_ARG);
+  CHECK(attend(3, RV_F32, mem, 64) == RV_E_ARG && attend(3, RV_F32, mem, 128, 64) == RV_E_ARG);
+  CHECK(attend(3, RV_F32, mem, 128, 128, 1) == RV_E_ARG);
   CHECK(g_launches == 0);
   const int32_t none[4] = {0, 0, 0, 0};
-  CHECK(rv_cache_attend(c, 0, pos, none, RV_F32, nullptr, 0, nullptr, 0, nullptr) == RV_OK && g_launches == 0);
+  CHECK(rv_cache_attend(c, 0, 4, pos, none, RV_F32, 0, 128, nullptr, 0, nullptr, 0, nullptr) == RV_OK && g_launches == 0);
   c->rows_cap = 2;
-  CHECK(rv_cache_attend(c, 0, pos, n, RV_F32, mem, 128, mem, 128, nullptr) == RV_E_CAPACITY);
+  CHECK(attend(3) == RV_E_CAPACITY);
   c->rows_cap = 2048;
 
   const int32_t s01[2] = {0, 1}, d23[2] = {2, 3}, d22[2] = {2, 2}, d24[2] = {2, 4}, l[2] = {100, 200}, l0[2] = {0, 1},

@@ -489,17 +489,22 @@ def test_arguments_of_the_binding(rv, gpu):
     rv.rv_cache_append(c.h, 0, [0] * 3, [1] * 3, q, k, k, q)
     for pos, n, a in (([0] * 2, [1] * 2, (q, k, k, q)), ([0] * 3, [1, 1], (q, k, k, q)),
                       ([0] * 3, [1, 1, 2], (q, k, k, q)), ([0] * 3, [1] * 3, (q, q, k, q)),
+                      ([0] * 3, [1] * 3, (q, q, q, q)), ([0] * 3, [1] * 3, (k, k, k, k)),
                       ([0] * 3, [1] * 3, (q, k.double(), k, q)), ([0] * 3, [1] * 3, (q, k, k.bfloat16(), q)),
                       ([0] * 3, [1] * 3, (q, k.T.contiguous().T, k, q)), ([0] * 3, [1] * 3, (q, k.cpu(), k, q)),
-                      ([0] * 3, [1] * 3, (q, k, k, q[:, :128]))):
-        with pytest.raises(ValueError):
+                      ([0] * 3, [1] * 3, (q, k, k, q[:, :128])), ([0] * 3, [1] * 3, (q, k, k, None))):
+        with pytest.raises((ValueError, rv.RVError)):
             rv.rv_cache_append(c.h, 0, pos, n, *a)
     for gain in (torch.ones(32, device="cuda"), torch.ones(64, device="cuda").double(),
                  torch.ones(128, device="cuda")[::2]):
         with pytest.raises(ValueError):
             rv.rv_cache_append(c.h, 0, [0] * 3, [1] * 3, q, k, k, q, q_gain=gain)
-    with pytest.raises(ValueError):
+    with pytest.raises(rv.RVError):
         rv.rv_cache_attend(c.h, 0, [0] * 3, [1] * 3, k, k)
+    with pytest.raises(ValueError):
+        rv.rv_cache_attend(c.h, 0, [0] * 3, [1] * 3, q, q.bfloat16())
+    with pytest.raises(rv.RVError):
+        rv.rv_cache_read(c.h, 0, [0] * 3, [1] * 3, q, q.clone())
     with pytest.raises(ValueError):
         rv.rv_cache_copy(c.h, [0, 1], [2], [1])
     with pytest.raises(rv.RVError):
