@@ -14,6 +14,9 @@ namespace {
 
 constexpr int kKB = kTile;
 
+// How a part is computed (kinds of rv_tiles.h): by k_share's workgroups of 512.
+enum { KIND_NONE = 0, KIND_FEW = 1, KIND_MANY = 2, KIND_MANY2 = 3 };
+
 // What one workgroup attends: keys [kbeg, kend) as table row `seq` reads them,
 // by queries q_begin.. of nq (query slots of one kv head).
 struct Unit {
@@ -94,11 +97,18 @@ RV_DEV int first_limit(const ShareArgs& a, const Unit& u) {
   return PART ? a.pos0[u.seq] + u.q_begin / (a.n_heads / a.n_kv) : 0x7fffffff;
 }
 
-// First element of tile t of (table row seq, kv head) in a plane of this layer.
+// Slot that holds tile t of table row seq, and the tile's first element there in
+// a plane of this layer.
+RV_DEV int tile_slot(const ShareArgs& a, int seq, int t) {
+  return a.own ? a.own[(size_t)seq * (a.kv_len / kKB) + t] : seq;
+}
+template <int HD>
+RV_DEV size_t tile_at(const ShareArgs& a, int slot, int kvh, int t) {
+  return ((size_t)(slot * a.n_kv + kvh) * a.kv_len + (size_t)t * kKB) * HD;
+}
 template <int HD>
 RV_DEV size_t tile_base(const ShareArgs& a, int seq, int kvh, int t) {
-  const int slot = a.own ? __builtin_amdgcn_readfirstlane(a.own[(size_t)seq * (a.kv_len / kKB) + t]) : seq;
-  return ((size_t)(slot * a.n_kv + kvh) * a.kv_len + (size_t)t * kKB) * HD;
+  return tile_at<HD>(a, __builtin_amdgcn_readfirstlane(tile_slot(a, seq, t)), kvh, t);
 }
 
 // B operands of one query: dims 32c + 8g .. +7 of chunk c as hi and lo planes.
@@ -149,14 +159,17 @@ RV_DEV size_t part_index(const ShareArgs& a, int slot, int row, int head) {
 }
 
 // Softmax weights of one query's scores of NB 16-key blocks: masks keys past
-// the limit, folds them into (m, l) and leaves 2^(s - m) in s.  Returns the
-// factor for what was summed before.  m follows the largest score only where one
-// exceeds it by more than kSlack, for the whole wave at once, so that most tiles
-// rescale nothing; weights then stay below 2^kSlack.  A wave whose queries all
-// see nothing yet keeps m = -inf, weights 0.
+// the limit, adds them to l (this lane's share of the sum) and leaves
+// 2^(s - m) in s.  m, the same in the query's four lanes, follows the largest
+// score only where one exceeds it by more than kSlack (for the whole wave at
+// once): most calls then need neither the lanes' maximum nor a rescale, and
+// weights stay below 2^kSlack.  Returns whether *rescale, the factor for what was
+// summed before, is to be applied.  A wave whose queries all see nothing yet
+// keeps m = -inf, weights 0.
 constexpr float kSlack = 6.0f;
 template <int NB>
-RV_DEV float softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, float sc, bool masked, float& m, float& l) {
+RV_DEV bool softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, float sc, bool masked, float& m, float& l,
+                         float* rescale) {
   float top = -INFINITY;
 #pragma unroll
   for (int t = 0; t < NB; ++t)
@@ -168,11 +181,11 @@ RV_DEV float softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, f
       }
       top = fmaxf(top, s[t][i]);
     }
-  top = rows4_max(top) * sc;
-  float rescale = 1.0f;
-  if (__any(top > m + kSlack)) {
-    const float m_new = fmaxf(m, top);
-    rescale = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+  const bool grew = __any(top * sc > m + kSlack);
+  if (grew) {
+    const float m_new = fmaxf(m, rows4_max(top) * sc);
+    *rescale = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+    l *= *rescale;
     m = m_new;
   }
   const float base = m == -INFINITY ? 0.f : m;
@@ -184,8 +197,8 @@ RV_DEV float softmax_step(f32x4_t (&s)[NB], int k0, int kend, int last, int g, f
       s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], sc, -base));
       sum += s[t][i];
     }
-  l = l * rescale + rows4_sum(sum);
-  return rescale;
+  l += sum;
+  return grew;
 }
 
 // P of two 16-key blocks as hi and lo B operands.
@@ -248,6 +261,7 @@ RV_DEV void take_out(u32x4 (&vh)[ND], u32x4 (&vl)[ND], int k0, int kend, const Q
       for (int i = 0; i < 4; ++i)
         if (seen[i] > 0.f) O[t][d0 + d][i] = __builtin_nanf("");
     }
+    __builtin_amdgcn_sched_barrier(0);  // one d tile's registers at a time
   }
 }
 
@@ -261,28 +275,37 @@ RV_DEV void take_out(u32x4 (&vh)[ND], u32x4 (&vl)[ND], int k0, int kend, const Q
 // / v_elem): a 64-key tile is four spans that go global -> LDS directly,
 // double-buffered.
 template <int HD, int PART, int TPW, bool QLO>
-__global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
+RV_DEV void attend_many(const ShareArgs& a, const Unit& u, uint16_t (&sm0)[4][kKB * HD], uint16_t (&sm1)[4][kKB * HD]) {
   constexpr int NW = 8, DC = HD / 32, DT = HD / 16, SPAN = kKB * HD;
   constexpr int UPW = 4 * SPAN / 512 / NW;  // 1 KiB pieces each wave copies, all of one span
-  __shared__ __attribute__((aligned(16))) uint16_t sm0[4][SPAN];
-  __shared__ __attribute__((aligned(16))) uint16_t sm1[4][SPAN];
-  Unit u;
-  if (!unit_of<PART>(a, blockIdx.x, u)) return;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
 
+  // This wave's share of a tile's copy: UPW pieces of 1 KiB of one span, which go
+  // out one by one between the products (all at once they keep the waves from
+  // their first products for the 1000 cycles that 64 KiB take to request).  The
+  // slot of the tile after the next is looked up a tile ahead.
   const int sp = w / 2, off = (w & 1) * (SPAN / 2);
   const uint16_t* plane = (const uint16_t*)(sp == 0 ? a.kc : sp == 1 ? a.kc2 : sp == 2 ? a.vc : a.vc2) + off;
-  auto fetch = [&](uint16_t(&sm)[4][SPAN], int k0) {
-    const uint16_t* src = plane + tile_base<HD>(a, u.seq, u.kvh, k0 / kKB);
-    auto* dst = (__attribute__((address_space(3))) char*)(&sm[0][0] + sp * SPAN + off);
-#pragma unroll
-    for (int i = 0; i < UPW; ++i)
-      __builtin_amdgcn_global_load_lds((const void*)(src + lane * 8 + i * 512),
-                                       (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
+  const int last_t = (u.kend - 1) / kKB;
+  int slot = tile_slot(a, u.seq, u.kbeg / kKB);
+  const uint16_t* src = nullptr;  // of the copy under way
+  auto next_copy = [&](int k0) {  // the copy of the tile at k0 begins
+    src = plane + tile_at<HD>(a, __builtin_amdgcn_readfirstlane(slot), u.kvh, k0 / kKB);
+    slot = tile_slot(a, u.seq, min(k0 / kKB + 1, last_t));
   };
-  fetch(sm0, u.kbeg);
+  auto copy_piece = [&](uint16_t(&sm)[4][SPAN], int i) {
+    __builtin_amdgcn_global_load_lds((const void*)(src + lane * 8 + i * 512),
+                                     (__attribute__((address_space(3))) void*)(&sm[0][0] + sp * SPAN + off + i * 512), 16,
+                                     0, 0);
+  };
+  next_copy(u.kbeg);
+#pragma unroll
+  for (int i = 0; i < UPW; ++i) copy_piece(sm0, i);
 
+  // of the two waves on a SIMD the first goes first, so that its products run
+  // while the other computes weights and the other way round
+  if (w < 4) __builtin_amdgcn_s_setprio(1);
   const int q0 = u.q_begin + 16 * TPW * w;
   const bool active = q0 < u.nq;
   const int first_last = first_limit<PART>(a, u);
@@ -303,62 +326,74 @@ __global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
     for (int d = 0; d < DT; ++d) O[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  auto tile = [&](const uint16_t(&sm)[4][SPAN], int k0) {
-    if (!active) return;
-    f32x4_t s[TPW][4];
+  // 32 keys at a time: scores, weights, products with V
+  static_assert(UPW == 2 * DC, "a piece of the copy per 32-dim chunk of each half");
+  auto tile = [&](const uint16_t(&sm)[4][SPAN], uint16_t(&other)[4][SPAN], int k_tile) {
+    const bool more = k_tile + kKB < u.kend;
+    if (more) next_copy(k_tile + kKB);
+    if (!active) {
+      if (more) {
 #pragma unroll
-    for (int t = 0; t < TPW; ++t)
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) s[t][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < DC; ++c) {
-      u32x4 kh[4], kl[4];
-#pragma unroll
-      for (int kb = 0; kb < 4; ++kb) {
-        kh[kb] = *(const u32x4*)(&sm[0][(kb * DC + c) * 512 + lane * 8]);
-        kl[kb] = *(const u32x4*)(&sm[1][(kb * DC + c) * 512 + lane * 8]);
+        for (int i = 0; i < UPW; ++i) copy_piece(other, i);
       }
+      return;
+    }
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      const int k0 = k_tile + 32 * half;
+      const uint16_t *kp = &sm[0][half * 2 * DC * 512 + lane * 8], *vp = &sm[2][half * DT * 512 + lane * 8];
+      f32x4_t s[TPW][2];
 #pragma unroll
       for (int t = 0; t < TPW; ++t)
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) s[t][kb] = mfma(kh[kb], __builtin_bit_cast(bf16x8_t, qh[t][c]), s[t][kb]);
+        for (int kb = 0; kb < 2; ++kb) s[t][kb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < TPW; ++t)
+      for (int c = 0; c < DC; ++c) {
+        u32x4 kh[2], kl[2];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) s[t][kb] = mfma(kl[kb], __builtin_bit_cast(bf16x8_t, qh[t][c]), s[t][kb]);
-      if constexpr (QLO) {
+        for (int kb = 0; kb < 2; ++kb) {
+          kh[kb] = *(const u32x4*)(kp + (kb * DC + c) * 512);
+          kl[kb] = *(const u32x4*)(kp + SPAN + (kb * DC + c) * 512);
+        }
 #pragma unroll
         for (int t = 0; t < TPW; ++t)
 #pragma unroll
-          for (int kb = 0; kb < 4; ++kb) s[t][kb] = mfma(kh[kb], __builtin_bit_cast(bf16x8_t, ql[t][c]), s[t][kb]);
+          for (int kb = 0; kb < 2; ++kb) s[t][kb] = mfma(kh[kb], __builtin_bit_cast(bf16x8_t, qh[t][c]), s[t][kb]);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) s[t][kb] = mfma(kl[kb], __builtin_bit_cast(bf16x8_t, qh[t][c]), s[t][kb]);
+        if constexpr (QLO) {
+#pragma unroll
+          for (int t = 0; t < TPW; ++t)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) s[t][kb] = mfma(kh[kb], __builtin_bit_cast(bf16x8_t, ql[t][c]), s[t][kb]);
+        }
+        if (more) copy_piece(other, half * DC + c);
       }
-    }
-    const bool masked = PART && (k0 + kKB > u.kend || k0 + kKB - 1 > first_last);
-#pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-      const float rescale = softmax_step<4>(s[t], k0, u.kend, q[t].last, g, a.scale_log2, masked, m[t], l[t]);
-      if (__any(rescale != 1.0f)) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) O[t][d] *= rescale;
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
+      const bool masked = PART && (k0 + 32 > u.kend || k0 + 31 > first_last);
       bf16x8_t ph[TPW], pl[TPW];
 #pragma unroll
-      for (int t = 0; t < TPW; ++t) split_p(s[t][2 * c], s[t][2 * c + 1], ph[t], pl[t]);
+      for (int t = 0; t < TPW; ++t) {
+        float rescale;
+        if (softmax_step<2>(s[t], k0, u.kend, q[t].last, g, a.scale_log2, masked, m[t], l[t], &rescale)) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) O[t][d] *= rescale;
+        }
+        split_p(s[t][0], s[t][1], ph[t], pl[t]);
+      }
       // four d tiles at a time: their operands, then the products in passes, so
       // that dependent MFMAs are 4 TPW apart
+      constexpr int ND = DT < 4 ? DT : 4;
 #pragma unroll
-      for (int d0 = 0; d0 < DT; d0 += DT < 4 ? DT : 4) {
-        constexpr int ND = DT < 4 ? DT : 4;
+      for (int d0 = 0; d0 < DT; d0 += ND) {
         u32x4 vh[ND], vl[ND];
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          vh[d] = *(const u32x4*)(&sm[2][(c * DT + d0 + d) * 512 + lane * 8]);
-          vl[d] = *(const u32x4*)(&sm[3][(c * DT + d0 + d) * 512 + lane * 8]);
+          vh[d] = *(const u32x4*)(vp + (d0 + d) * 512);
+          vl[d] = *(const u32x4*)(vp + SPAN + (d0 + d) * 512);
         }
-        if (masked && any_not_finite<ND>(vh)) take_out<ND, TPW, DT>(vh, vl, k0 + 32 * c, u.kend, q, g, O, d0);
+        if (masked && any_not_finite<ND>(vh)) take_out<ND, TPW, DT>(vh, vl, k0, u.kend, q, g, O, d0);
 #pragma unroll
         for (int t = 0; t < TPW; ++t)
 #pragma unroll
@@ -375,24 +410,23 @@ __global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
     }
   };
 
-  // at the top of each half only the copy of the tile about to be used is in
+  // at the top of each step only the copy of the tile about to be used is in
   // flight; after the barrier every wave has finished the one before, whose
   // buffer takes the next
   for (int k0 = u.kbeg; k0 < u.kend; k0 += 2 * kKB) {
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (k0 + kKB < u.kend) fetch(sm1, k0 + kKB);
-    tile(sm0, k0);
+    tile(sm0, sm1, k0);
     if (k0 + kKB >= u.kend) break;
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (k0 + 2 * kKB < u.kend) fetch(sm0, k0 + 2 * kKB);
-    tile(sm1, k0 + kKB);
+    tile(sm1, sm0, k0 + kKB);
   }
 
   // lane holds O^T[d = 16t + 4g + i][query lane%16]
 #pragma unroll
   for (int t = 0; t < TPW; ++t) {
+    l[t] = rows4_sum(l[t]);
     if (!q[t].valid) continue;
     if (a.direct) {
       const float inv = 1.0f / l[t];
@@ -414,20 +448,29 @@ __global__ __launch_bounds__(512) void k_share_many(ShareArgs a) {
 // Decode steps: the 8 waves share the 16 queries and split the keys, wave w
 // taking tiles w, w + 8, ... of KT keys straight to registers; their states
 // merge in LDS.
-template <int HD, int PART>
-__global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
+// red: 8 x 16 x HD values in LDS, 16-byte columns xor-ed with the query so that
+// the 16 queries of a column lie in different banks; red_ml: 2 x 8 x 16.
+template <int HD, int PART, bool QLO>
+RV_DEV void attend_few(const ShareArgs& a, const Unit& u, float* red, float* red_ml) {
   constexpr int KT = HD == 128 ? 32 : 64, NW = 8, NB = KT / 16, NC = KT / 32, DC = HD / 32, DT = HD / 16;
-  __shared__ __attribute__((aligned(16))) float red_o[NW][16][HD + 4];
-  __shared__ float red_m[NW][16], red_l[NW][16];
-  Unit u;
-  if (!unit_of<PART>(a, blockIdx.x, u)) return;
+  constexpr int COLS = HD / 4 < 16 ? HD / 4 : 16;  // columns that the xor permutes
+  auto at_red = [&](int wave, int query, int col) {
+    return (f32x4_t*)(red + ((wave * 16 + query) * (HD / 4) + (col ^ (query & (COLS - 1)))) * 4);
+  };
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  const Query q[1] = {query_of<PART>(a, u, u.q_begin + (lane & 15))};
+  const int first_last = first_limit<PART>(a, u);
+  u32x4 qh[DC], ql[DC];
+  load_query<HD>(a, q[0], g, qh, ql);
 
   u32x4 k[2][NB][DC], v[2][NC][DT];
   // tiles past the last load that one again and are not used
   const int last_tile = u.kbeg + (u.kend - 1 - u.kbeg) / KT * KT;
-  auto at = [&](int k0) { return tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + (size_t)(k0 % kKB) * HD + lane * 8; };
+  // (uniform offsets: the loads then need one lane offset and no 64-bit addresses)
+  auto at = [&](int k0) { return tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + (size_t)(k0 % kKB) * HD; };
+  const unsigned lane16 = lane * 16;
   auto load_k = [&](size_t o) {
 #pragma unroll
     for (int pl = 0; pl < 2; ++pl)
@@ -435,7 +478,7 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
       for (int t = 0; t < NB; ++t)
 #pragma unroll
         for (int c = 0; c < DC; ++c)
-          k[pl][t][c] = *(const u32x4*)((const uint16_t*)(pl ? a.kc2 : a.kc) + o + (t * DC + c) * 512);
+          k[pl][t][c] = *(const u32x4*)((const char*)((const uint16_t*)(pl ? a.kc2 : a.kc) + o + (t * DC + c) * 512) + lane16);
   };
   auto load_v = [&](size_t o) {
 #pragma unroll
@@ -444,19 +487,17 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          v[pl][c][d] = *(const u32x4*)((const uint16_t*)(pl ? a.vc2 : a.vc) + o + (c * DT + d) * 512);
+          v[pl][c][d] = *(const u32x4*)((const char*)((const uint16_t*)(pl ? a.vc2 : a.vc) + o + (c * DT + d) * 512) + lane16);
   };
   int k0 = u.kbeg + w * KT;
   size_t next = at(min(k0, last_tile));
-  if (k0 < u.kend) {
-    load_k(next);
-    load_v(next);
-  }
+  if (k0 >= u.kend) next = at(last_tile);  // a wave without tiles loads the last one and uses it not
+  // the order of the loop: K, then V, so that the wait for K leaves V in flight
+  load_k(next);
+  __builtin_amdgcn_sched_barrier(0);
+  load_v(next);
+  __builtin_amdgcn_sched_barrier(0);
   next = at(min(k0 + NW * KT, last_tile));
-  const Query q[1] = {query_of<PART>(a, u, u.q_begin + (lane & 15))};
-  const int first_last = first_limit<PART>(a, u);
-  u32x4 qh[DC], ql[DC];
-  load_query<HD>(a, q[0], g, qh, ql);
   float m = -INFINITY, l = 0.f;
   f32x4_t O[1][DT];
 #pragma unroll
@@ -471,16 +512,21 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
       const bf16x8_t h = __builtin_bit_cast(bf16x8_t, qh[c]), lo = __builtin_bit_cast(bf16x8_t, ql[c]);
 #pragma unroll
       for (int t = 0; t < NB; ++t) s[t] = mfma(k[0][t][c], h, s[t]);
+      if constexpr (QLO) {
 #pragma unroll
-      for (int t = 0; t < NB; ++t) s[t] = mfma(k[0][t][c], lo, s[t]);
+        for (int t = 0; t < NB; ++t) s[t] = mfma(k[0][t][c], lo, s[t]);
+      }
 #pragma unroll
       for (int t = 0; t < NB; ++t) s[t] = mfma(k[1][t][c], h, s[t]);
     }
+    __builtin_amdgcn_sched_barrier(0);  // the next operands replace these: none are loaded before their last use
     load_k(next);
     const bool masked = k0 + KT > u.kend || k0 + KT - 1 > first_last;
-    const float rescale = softmax_step<NB>(s, k0, u.kend, q[0].last, g, a.scale_log2, masked, m, l);
+    float rescale;
+    if (softmax_step<NB>(s, k0, u.kend, q[0].last, g, a.scale_log2, masked, m, l, &rescale)) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) O[0][d] *= rescale;
+      for (int d = 0; d < DT; ++d) O[0][d] *= rescale;
+    }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       bf16x8_t ph, pl;
@@ -494,16 +540,18 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) O[0][d] = mfma(v[1][c][d], ph, O[0][d]);
     }
+    __builtin_amdgcn_sched_barrier(0);
     load_v(next);
     next = at(min(k0 + 2 * NW * KT, last_tile));
   }
 
   // merge the waves: one without tiles has m = -inf, l = 0, O = 0
+  l = rows4_sum(l);
 #pragma unroll
-  for (int d = 0; d < DT; ++d) *(f32x4_t*)&red_o[w][lane & 15][16 * d + 4 * g] = O[0][d];
+  for (int d = 0; d < DT; ++d) *at_red(w, lane & 15, 4 * d + g) = O[0][d];
   if (g == 0) {
-    red_m[w][lane & 15] = m;
-    red_l[w][lane & 15] = l;
+    red_ml[w * 16 + (lane & 15)] = m;
+    red_ml[(NW + w) * 16 + (lane & 15)] = l;
   }
   __syncthreads();
   const int oq = tid / (HD / 4), od = tid % (HD / 4) * 4;
@@ -512,13 +560,13 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
   if (!oqr.valid) return;
   float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int i = 0; i < NW; ++i) M = fmaxf(M, red_m[i][oq]);
+  for (int i = 0; i < NW; ++i) M = fmaxf(M, red_ml[i * 16 + oq]);
   f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
-    const float f = red_m[i][oq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_m[i][oq] - M);
-    L += red_l[i][oq] * f;
-    x += *(const f32x4_t*)&red_o[i][oq][od] * f;
+    const float f = red_ml[i * 16 + oq] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(red_ml[i * 16 + oq] - M);
+    L += red_ml[(NW + i) * 16 + oq] * f;
+    x += *at_red(i, oq, od / 4) * f;
   }
   if (a.direct) {
     put_out4<RV_BF16>(a, HD, oqr.row, oqr.head, od, x * (1.0f / L));
@@ -530,6 +578,39 @@ __global__ __launch_bounds__(512) void k_share_few(ShareArgs a) {
     a.part_ml[2 * e] = M;
     a.part_ml[2 * e + 1] = L;
   }
+}
+
+// ----------------------------------------------------------- bf16, one launch for both parts
+// Shared keys are compute (many queries a key), own keys of decode steps HBM (few
+// queries a key), so workgroups of the two parts run side by side.  Where the own
+// part fits beside the last round of the shared part, the shared part goes first;
+// else half of the chip starts with the one and half with the other (runs of 8
+// workgroups, one per XCD: lead_sh of the shared part, lead_own of the own, the
+// rest of the shared, the rest of the own).  SH, OW: kinds of the parts.
+template <int HD, int KIND, int PART, bool QLO>
+RV_DEV void attend_part(const ShareArgs& a, int x, uint16_t (&sm0)[4][kKB * HD], uint16_t (&sm1)[4][kKB * HD]) {
+  Unit u;
+  if (!unit_of<PART>(a, x, u)) return;
+  if constexpr (KIND == KIND_FEW) attend_few<HD, PART, QLO>(a, u, (float*)&sm0[0][0], (float*)&sm1[0][0]);
+  else if constexpr (KIND == KIND_MANY) attend_many<HD, PART, 1, QLO>(a, u, sm0, sm1);
+  else if constexpr (KIND == KIND_MANY2) attend_many<HD, PART, 2, QLO>(a, u, sm0, sm1);
+}
+template <int HD, int SH, int OW, bool QLO>
+__global__ __launch_bounds__(512) void k_share(ShareArgs a) {
+  __shared__ __attribute__((aligned(16))) uint16_t sm0[4][kKB * HD];
+  __shared__ __attribute__((aligned(16))) uint16_t sm1[4][kKB * HD];
+  int x = blockIdx.x;
+  if constexpr (SH != KIND_NONE) {
+    const int j = x / 8, lead = a.lead_sh + a.lead_own;
+    const bool sh = j < a.lead_sh || (j >= lead && j < a.runs_sh + a.lead_own);
+    const int run = j < a.lead_sh ? j : j < lead ? j - a.lead_sh : sh ? j - a.lead_own : j - a.runs_sh;
+    x = run * 8 + x % 8;
+    if (sh) {
+      attend_part<HD, SH, 0, QLO>(a, x, sm0, sm1);
+      return;
+    }
+  }
+  attend_part<HD, OW, 1, QLO>(a, x, sm0, sm1);
 }
 
 // As take_out, for four keys of an fp32 cache, where infinities keep their sign.
@@ -603,9 +684,11 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
         for (int i = 0; i < 4; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[c][i], qv[c][i], s[t], 0, 0, 0);
     }
     const bool masked = k0 + kKB > u.kend || k0 + kKB - 1 > first_last;
-    const float rescale = softmax_step<4>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l);
+    float rescale;
+    if (softmax_step<4>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l, &rescale)) {
 #pragma unroll
-    for (int t = 0; t < DC; ++t) o[t] *= rescale;
+      for (int t = 0; t < DC; ++t) o[t] *= rescale;
+    }
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -633,6 +716,7 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
         for (int e = 0; e < DC; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], s[t][i], o[e], 0, 0, 0);
       }
   }
+  l = rows4_sum(l);
   if (!q.valid) return;
   // lane holds dims (4g + i) DC + t of its query: a run of 4 DC
   const size_t e = part_index(a, u.slot, q.row, q.head);
@@ -697,27 +781,51 @@ __global__ __launch_bounds__(256) void k_share_merge(ShareArgs a) {
 }
 
 template <int HD, int PART>
-hipError_t launch_part(int dtype, const ShareArgs& a, hipStream_t st) {
-  const SharePart& sp = PART ? a.p.own : a.p.sh;
-  const size_t units = (size_t)sp.ns * a.n_kv * (PART ? a.p.nseq : a.p.groups);
-  const size_t grid = (units + 7) / 8 * 8 * sp.nqg;
-  if (!grid) return hipSuccess;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (dtype == RV_F32) k_share_f32<HD, PART><<<(unsigned)grid, 64, 0, st>>>(a);
-  else if (sp.qpw == 16) k_share_few<HD, PART><<<(unsigned)grid, 512, 0, st>>>(a);
-  else if (sp.qpw == 128 && a.q_kind == RV_BF16) k_share_many<HD, PART, 1, false><<<(unsigned)grid, 512, 0, st>>>(a);
-  else if (sp.qpw == 128) k_share_many<HD, PART, 1, true><<<(unsigned)grid, 512, 0, st>>>(a);
-  else if (a.q_kind == RV_BF16) k_share_many<HD, PART, 2, false><<<(unsigned)grid, 512, 0, st>>>(a);
-  else k_share_many<HD, PART, 2, true><<<(unsigned)grid, 512, 0, st>>>(a);
+hipError_t launch_f32(const ShareArgs& a, int runs, hipStream_t st) {
+  if (runs) k_share_f32<HD, PART><<<(unsigned)runs * 8, 64, 0, st>>>(a);
   return hipGetLastError();
 }
+
+template <int HD, int SH, int OW>
+void launch_kinds(const ShareArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)(a.runs_sh + a.runs_own) * 8;
+  if (a.q_kind == RV_BF16) k_share<HD, SH, OW, false><<<grid, 512, 0, st>>>(a);
+  else k_share<HD, SH, OW, true><<<grid, 512, 0, st>>>(a);
+}
+
+int kind_of(const SharePart& p) { return p.qpw == 16 ? KIND_FEW : p.qpw == 128 ? KIND_MANY : KIND_MANY2; }
+
+// Workgroups of a part, in runs of 8.
+size_t part_runs(const SharePart& p, int n, int n_kv) { return ((size_t)p.ns * n_kv * n + 7) / 8 * p.nqg; }
 
 template <int HD>
 hipError_t launch_all(int dtype, ShareArgs& a, hipStream_t st) {
   a.direct = a.p.groups == 0 && a.p.own.ns == 1;
-  if (a.p.groups)
-    if (hipError_t e = launch_part<HD, 0>(dtype, a, st); e != hipSuccess) return e;
-  if (hipError_t e = launch_part<HD, 1>(dtype, a, st); e != hipSuccess) return e;
+  const size_t sh = a.p.groups ? part_runs(a.p.sh, a.p.groups, a.n_kv) : 0, own = part_runs(a.p.own, a.p.nseq, a.n_kv);
+  if ((sh + own) * 8 > 0x7fffffff) return hipErrorInvalidValue;
+  a.runs_sh = (int)sh;
+  a.runs_own = (int)own;
+  a.lead_sh = a.p.own_last ? a.runs_sh : std::min(a.runs_sh, 16);
+  a.lead_own = a.p.own_last ? 0 : a.runs_own / 2;
+  if (dtype == RV_F32) {
+    if (hipError_t e = launch_f32<HD, 0>(a, a.runs_sh, st); e != hipSuccess) return e;
+    if (hipError_t e = launch_f32<HD, 1>(a, a.runs_own, st); e != hipSuccess) return e;
+  } else {
+    const int kinds = (sh ? kind_of(a.p.sh) : KIND_NONE) * 4 + kind_of(a.p.own);
+    switch (kinds) {
+      case KIND_NONE * 4 + KIND_FEW: launch_kinds<HD, KIND_NONE, KIND_FEW>(a, st); break;
+      case KIND_FEW * 4 + KIND_FEW: launch_kinds<HD, KIND_FEW, KIND_FEW>(a, st); break;
+      case KIND_MANY * 4 + KIND_FEW: launch_kinds<HD, KIND_MANY, KIND_FEW>(a, st); break;
+      case KIND_MANY2 * 4 + KIND_FEW: launch_kinds<HD, KIND_MANY2, KIND_FEW>(a, st); break;
+      case KIND_NONE * 4 + KIND_MANY: launch_kinds<HD, KIND_NONE, KIND_MANY>(a, st); break;
+      case KIND_MANY * 4 + KIND_MANY: launch_kinds<HD, KIND_MANY, KIND_MANY>(a, st); break;
+      case KIND_MANY2 * 4 + KIND_MANY: launch_kinds<HD, KIND_MANY2, KIND_MANY>(a, st); break;
+      case KIND_NONE * 4 + KIND_MANY2: launch_kinds<HD, KIND_NONE, KIND_MANY2>(a, st); break;
+      case KIND_MANY2 * 4 + KIND_MANY2: launch_kinds<HD, KIND_MANY2, KIND_MANY2>(a, st); break;
+      default: return hipErrorInvalidValue;
+    }
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   if (a.direct) return hipSuccess;
   int longest = 0;
   for (int b = 0; b < a.p.nseq; ++b) longest = std::max(longest, a.row0[b + 1] - a.row0[b]);

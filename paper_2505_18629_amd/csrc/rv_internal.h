@@ -302,8 +302,9 @@ struct ShareArgs {
   int q_kind, o_kind;
   int n_heads, n_kv, kv_len;
   float scale_log2;
-  int part;              // 0: shared keys, 1: the sequences' own keys (the launcher's)
-  int direct;            // one run and no groups: the output is final
+  int direct;            // one run and no groups: the output is final (this and the next are the launcher's)
+  int runs_sh, runs_own;  // workgroups of the two parts, in runs of 8
+  int lead_sh, lead_own;  // how many of each start first
   int pos0[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1];
   SharePlan p;
 };

@@ -5,6 +5,7 @@
 // alone (the host checks under tests/).
 #pragma once
 #include <algorithm>
+#include <cmath>
 #include <cstddef>
 #include <cstdint>
 #include <cstring>
@@ -215,6 +216,7 @@ struct SharePart {
 
 struct SharePlan {
   int nseq = 0, rows = 0, groups = 0;
+  bool own_last = false;         // the own part fits beside the last round of the shared part
   SharePart sh, own;
   uint8_t group_of[kMaxSlots];   // 255: none
   uint8_t member[kMaxSlots];     // members, group after group
@@ -273,55 +275,63 @@ inline void plan_groups(const TileOwners& tl, const int32_t* pos0, const int32_t
   }
 }
 
-// One unit of a part: `keys` keys against `queries` queries of a kv head.
+// One unit of a part before it is cut into runs: `keys` keys against `queries`
+// queries of a kv head.
 struct ShareUnit {
   int keys, queries;
 };
 
-// Run length of one part: the cheapest estimate over a few run counts, within
-// max_ns runs.  One run only where `single` asks for the whole part in one.
-inline SharePart plan_part(bool bf16, const ShareUnit* u, int n, int n_kv, int hd, int max_ns) {
-  SharePart s;
-  int kmax = 0, qmax = 0;
-  for (int i = 0; i < n; ++i) {
-    kmax = std::max(kmax, u[i].keys);
-    qmax = std::max(qmax, u[i].queries);
-  }
-  if (!kmax || !qmax) return s;
-  s.qpw = !bf16 || qmax <= 16 ? 16 : qmax <= 128 ? 128 : 256;
-  s.nqg = (qmax + s.qpw - 1) / s.qpw;
-  static const int counts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80};
-  double best = 0;
-  for (int ns : counts) {
-    if (ns > max_ns || (ns > 1 && (ns - 1) * kTile >= kmax)) break;
-    const int ks = ((kmax + ns - 1) / ns + kTile - 1) / kTile * kTile;
-    long long wgs = 0, keys = 0;
-    for (int i = 0; i < n; ++i) {
-      wgs += (long long)((u[i].keys + ks - 1) / ks) * ((u[i].queries + s.qpw - 1) / s.qpw) * n_kv;
-      keys += u[i].keys;
-    }
-    double t;
-    if (!bf16) {  // a wave per workgroup, eight resident on a CU
-      t = (double)((wgs + 2047) / 2048) * (ks / kTile + 1) * 3.0 * hd / 128;
-    } else if (s.qpw == 16) {
-      const double stream = (double)keys * n_kv * 8 * hd / 5.5e6;
-      t = std::max((double)((wgs + 255) / 256) * std::min(ks, kmax) * 8 * hd / 4.5e4, stream);
-    } else {
-      t = (double)((wgs + 255) / 256) * (ks / kTile + 2) * (s.qpw == 128 ? 2.2 : 3.8) * hd / 128;
-    }
-    const int runs = (kmax + ks - 1) / ks;
-    t += 0.05 * runs;
-    if (!s.ks || t < best) {
-      best = t;
-      s.ks = ks;
-      s.ns = runs;
-    }
-  }
-  return s;
+// A part cut into `ns` runs of ks keys: its workgroups, the sum of their times
+// and the longest (us).
+struct ShareCut {
+  int ks, ns;
+  long long wgs;
+  double sum, longest;
+};
+
+constexpr int kCutCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80};
+constexpr int kCuts = sizeof kCutCounts / sizeof kCutCounts[0];
+
+// us of a workgroup that attends `keys` keys: prologue, epilogue and latencies,
+// then the keys at its rate (head_dim 128; others in proportion).
+inline double share_wg_us(bool bf16, int qpw, int keys, int hd) {
+  const double f = hd / 128.0;
+  if (!bf16) return 2.5 + (keys + kTile - 1) / kTile * 1.5 * f;      // a wave of 16 queries
+  if (qpw == 16) return 4.0 + keys * 8.0 * hd / 4.5e4;               // what one CU draws
+  return 5.0 + (keys + kTile - 1) / kTile * (qpw == 128 ? 3.2 : 5.2) * f;
 }
 
-// Launch shape of a call.  part_entries: (slot, row, head) results that the
-// partial buffer holds; n_heads * rows <= part_entries / 2 always fits.
+// The cuts of a part worth trying, within max_ns runs; their number.
+inline int cut_part(bool bf16, const ShareUnit* u, int n, int n_kv, int hd, int qpw, int max_ns, ShareCut* out) {
+  int kmax = 0, m = 0;
+  for (int i = 0; i < n; ++i) kmax = std::max(kmax, u[i].keys);
+  for (int ns : kCutCounts) {
+    if (ns > max_ns || (ns > 1 && (ns - 1) * kTile >= kmax)) break;
+    ShareCut c{};
+    c.ks = ((kmax + ns - 1) / ns + kTile - 1) / kTile * kTile;
+    c.ns = (kmax + c.ks - 1) / c.ks;
+    if (m && out[m - 1].ns == c.ns) continue;
+    const double whole = share_wg_us(bf16, qpw, c.ks, hd);
+    for (int i = 0; i < n; ++i) {
+      const long long w = (long long)((u[i].queries + qpw - 1) / qpw) * n_kv;
+      const int full = u[i].keys / c.ks, rest = u[i].keys % c.ks;
+      c.wgs += w * (full + (rest > 0));
+      c.sum += (double)w * (full * whole + (rest ? share_wg_us(bf16, qpw, rest, hd) : 0));
+    }
+    c.longest = share_wg_us(bf16, qpw, std::min(c.ks, kmax), hd);
+    out[m++] = c;
+  }
+  return m;
+}
+
+// Launch shape of a call.  part_entries: (run, row, head) results that the
+// partial buffer holds; n_heads * rows <= part_entries / 2 always fits.  Both
+// parts run in one launch (fp32 caches: two).  The shared part's workgroups are
+// the long ones: they take whole rounds of the CUs, the own part's fill what
+// those leave and then add their share and half of one; every run costs its
+// results' write and the merge's read.  (64 continuations of 32768 keys at the
+// 70B shape: one round of 256 workgroups; with one and a half, 384, the same
+// work took 253 instead of 184 us.)
 inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, const int32_t* row0, int n_heads, int n_kv,
                        int hd, size_t part_entries, SharePlan& p) {
   const int B = tl.B, G = n_heads / n_kv;
@@ -329,20 +339,51 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
   p.rows = row0[B];
   plan_groups(tl, pos0, row0, p);
   const int fit = (int)std::min<size_t>(kMergeSlots, part_entries / ((size_t)p.rows * n_heads));
-  ShareUnit u[kMaxSlots];
-  int n = 0;
-  p.sh = SharePart{};
-  if (p.groups) {
-    for (int g = 0; g < p.groups; ++g)
-      u[n++] = ShareUnit{p.tiles[g] * kTile, (p.first[g + 1] - p.first[g]) * p.rmax[g] * G};
-    p.sh = plan_part(bf16, u, n, n_kv, hd, std::max(1, fit / 2));
-  }
-  n = 0;
+  ShareUnit own[kMaxSlots], sh[kShareGroups];
+  int n = 0, most = 0, most_sh = 0;
+  long long bytes = 0;
   for (int b = 0; b < B; ++b) {
     const int r = row0[b + 1] - row0[b];
     if (!r) continue;
     const int t0 = p.group_of[b] == 255 ? 0 : p.tiles[p.group_of[b]];
-    u[n++] = ShareUnit{pos0[b] + r - t0 * kTile, r * G};
+    own[n++] = ShareUnit{pos0[b] + r - t0 * kTile, r * G};
+    most = std::max(most, r * G);
+    bytes += own[n - 1].keys;
   }
-  p.own = plan_part(bf16, u, n, n_kv, hd, std::max(1, fit - p.sh.ns));
+  for (int g = 0; g < p.groups; ++g) {
+    sh[g] = ShareUnit{p.tiles[g] * kTile, (p.first[g + 1] - p.first[g]) * p.rmax[g] * G};
+    most_sh = std::max(most_sh, sh[g].queries);
+    bytes += sh[g].keys;
+  }
+  // queries per workgroup: never fewer of the shared part than of the own part
+  auto qpw = [&](int q) { return !bf16 || q <= 16 ? 16 : q <= 128 ? 128 : 256; };
+  p.own = SharePart{qpw(most), 0, 0, 0};
+  p.sh = SharePart{std::max(p.own.qpw, qpw(most_sh)), 0, 0, 0};
+  p.own.nqg = (most + p.own.qpw - 1) / p.own.qpw;
+  p.sh.nqg = (most_sh + p.sh.qpw - 1) / p.sh.qpw;
+  ShareCut a[kCuts], c[kCuts];
+  const int na = p.groups ? cut_part(bf16, sh, p.groups, n_kv, hd, p.sh.qpw, std::max(1, fit / 2), a) : 1;
+  if (!p.groups) a[0] = ShareCut{};
+  const int nc = cut_part(bf16, own, n, n_kv, hd, p.own.qpw, std::max(1, fit - (p.groups ? 1 : 0)), c);
+  const double stream = (double)bytes * n_kv * 8 * hd / 5.2e6, slots = bf16 ? 256 : 2048;
+  double best = 0;
+  for (int i = 0; i < na; ++i)
+    for (int j = 0; j < nc; ++j) {
+      const int runs = a[i].ns + c[j].ns;
+      if (runs > fit && (i || j)) continue;
+      const double rounds = std::ceil(a[i].wgs / slots), gap = rounds * slots * a[i].longest - a[i].sum;
+      double t = rounds * a[i].longest;
+      if (!rounds) t = c[j].wgs <= slots ? c[j].longest : c[j].sum / slots + c[j].longest / 2;
+      else if (c[j].sum > gap) t += (c[j].sum - gap) / slots + c[j].longest / 2;
+      t = std::max(std::max(t, c[j].longest), stream);
+      if (runs > 1) t += 5.0 + 0.1 * runs + (double)runs * p.rows * n_heads * hd * 8 / 3.5e6;
+      if ((!i && !j) || t < best) {
+        best = t;
+        p.sh.ks = a[i].ks;
+        p.sh.ns = a[i].ns;
+        p.own.ks = c[j].ks;
+        p.own.ns = c[j].ns;
+        p.own_last = c[j].sum <= gap;
+      }
+    }
 }
