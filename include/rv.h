@@ -260,8 +260,11 @@ typedef struct {
   const void *d_q, *d_k, *d_v;        /* d_q may be NULL */
   void* d_q_out;                      /* queries, normalised and rotated; may be d_q; NULL with d_q */
   int64_t ld_q, ld_k, ld_v, ld_q_out;
-  const float *d_q_gain, *d_k_gain;   /* [head_dim] fp32, or NULL: that side is not normalised */
+  const float *d_q_gain, *d_k_gain;   /* [head_dim] fp32 at multiples of 16 bytes, or NULL: that side is not normalised */
 } rv_rows;
+
+/* What the rows of a call must fit: h_dims[0..3] = batch, n_heads, n_kv_heads, head_dim. */
+rv_status rv_cache_dims(const rv_cache* c, int32_t* h_dims);
 
 /* Writes rows of K and V to one layer of the cache.  With gains, each head x of
  * a query or key is first normalised, y = x / sqrt(mean(x^2) + rms_eps) * g;

@@ -147,6 +147,15 @@ def _stream(stream) -> Optional[int]:
     return torch.cuda.current_stream().cuda_stream
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # what current_stream asks, without its 3 us
+
+
+def _stream_on(device: int, stream) -> Optional[int]:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device)
+    return _stream(stream)
+
+
 def _host_i32(vals: Sequence[int]):
     arr = np.ascontiguousarray(np.asarray(vals, dtype=np.int32))
     return arr, arr.ctypes.data_as(_P_i32)
@@ -280,18 +289,17 @@ def _spans(positions, counts):
     return batch, pos, n
 
 
-def _row_tensors(a, *others) -> int:
+def _row_tensors(here: int, a, *others) -> int:
     """Type of the rows of tensors of one type on the current device, each dense within a row."""
-    kind = _ROW_TYPES.get(a.dtype)
+    dtype, rows = a.dtype, a.shape[0]
+    kind = _ROW_TYPES.get(dtype)
     if kind is None:
-        raise ValueError(f"rows must be float32 or bfloat16, not {a.dtype}")
-    here, rows = torch.cuda.current_device(), a.shape[0]
+        raise ValueError(f"rows must be float32 or bfloat16, not {dtype}")
     for t in (a,) + others:
-        if t.dim() != 2 or t.shape[0] != rows or t.dtype != a.dtype or (t.stride(1) != 1 and rows):
-            raise ValueError(f"expected {rows} rows of {a.dtype}, dense within a row, got {tuple(t.shape)} of {t.dtype} "
-                             f"with strides {t.stride()}")
-        if t.get_device() != here:
-            raise ValueError(f"rows on {t.device}, the current device is cuda:{here}")
+        if t.dtype != dtype or t.get_device() != here or t.dim() != 2 or t.shape[0] != rows or \
+                (t.stride(1) != 1 and rows):
+            raise ValueError(f"expected {rows} rows of {dtype} on cuda:{here} (the current device), dense within a row, "
+                             f"got {tuple(t.shape)} of {t.dtype} with strides {t.stride()} on {t.device}")
     return kind
 
 
@@ -315,50 +323,53 @@ def rv_cache_dims(cache: int):
 def rv_cache_append(cache: int, layer: int, positions, counts, q, k, v, q_out, q_gain=None, k_gain=None,
                     rotate: bool = True, stream=None) -> None:
     """q and q_out may be None together; q_out may be q."""
+    here = torch.cuda.current_device()
     batch, pos, n = _spans(positions, counts)
     rows, width = k.shape
     if v.shape != k.shape or (q is None) != (q_out is None) or (q is not None and q.shape != q_out.shape):
         raise ValueError("k and v, and q and its output, have the same shape")
     hd = 0 if q_gain is None and k_gain is None else rv_cache_dims(cache)[3]
     if q is None:
-        a = rv_rows(_row_tensors(k, v), rotate, rows, 0, width, None, k.data_ptr(), v.data_ptr(), None, 0, k.stride(0),
+        a = rv_rows(_row_tensors(here, k, v), rotate, rows, 0, width, None, k.data_ptr(), v.data_ptr(), None, 0, k.stride(0),
                     v.stride(0), 0, _gain(q_gain, hd), _gain(k_gain, hd))
     else:
-        a = rv_rows(_row_tensors(k, v, q, q_out), rotate, rows, q.shape[1], width, q.data_ptr(), k.data_ptr(),
+        a = rv_rows(_row_tensors(here, k, v, q, q_out), rotate, rows, q.shape[1], width, q.data_ptr(), k.data_ptr(),
                     v.data_ptr(), q_out.data_ptr(), q.stride(0), k.stride(0), v.stride(0), q_out.stride(0),
                     _gain(q_gain, hd), _gain(k_gain, hd))
-    _check(_lib.rv_cache_append(cache, layer, batch, pos, n, ctypes.byref(a), _stream(stream)))
+    _check(_lib.rv_cache_append(cache, layer, batch, pos, n, ctypes.byref(a), _stream_on(here, stream)))
 
 
 def rv_cache_read(cache: int, layer: int, positions, counts, k, v, stream=None) -> None:
+    here = torch.cuda.current_device()
     batch, pos, n = _spans(positions, counts)
     if v.shape != k.shape:
         raise ValueError("k and v have the same shape")
-    kind = _row_tensors(k, v)
+    kind = _row_tensors(here, k, v)
     _check(_lib.rv_cache_read(cache, layer, batch, pos, n, kind, k.shape[0], k.shape[1], k.data_ptr(), k.stride(0),
-                              v.data_ptr(), v.stride(0), _stream(stream)))
+                              v.data_ptr(), v.stride(0), _stream_on(here, stream)))
 
 
 def rv_cache_copy(cache: int, src, dst, lengths, stream=None) -> None:
     (a, s), (b, d), (c, n) = _i32_bytes(src), _i32_bytes(dst), _i32_bytes(lengths)
     if a != b or a != c:
         raise ValueError(f"{a} sources, {b} destinations and {c} lengths")
-    _check(_lib.rv_cache_copy(cache, a, s, d, n, _stream(stream)))
+    _check(_lib.rv_cache_copy(cache, a, s, d, n, _stream_on(torch.cuda.current_device(), stream)))
 
 
 def rv_cache_fork(cache: int, src: int, length: int, dst, stream=None) -> None:
     n, d = _i32_bytes(dst)
-    _check(_lib.rv_cache_fork(cache, src, length, n, d, _stream(stream)))
+    _check(_lib.rv_cache_fork(cache, src, length, n, d, _stream_on(torch.cuda.current_device(), stream)))
 
 
 def rv_cache_attend(cache: int, layer: int, positions, counts, q, out, stream=None) -> None:
     """out may be q."""
+    here = torch.cuda.current_device()
     batch, pos, n = _spans(positions, counts)
     if out.shape != q.shape:
         raise ValueError("q and the output have the same shape")
-    kind = _row_tensors(q, out)
+    kind = _row_tensors(here, q, out)
     _check(_lib.rv_cache_attend(cache, layer, batch, pos, n, kind, q.shape[0], q.shape[1], q.data_ptr(), q.stride(0),
-                                out.data_ptr(), out.stride(0), _stream(stream)))
+                                out.data_ptr(), out.stride(0), _stream_on(here, stream)))
 
 
 def rv_model_qk_norm(model: int, q_gain, k_gain) -> None:

@@ -116,12 +116,13 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
       load8<RV_F32>(a.rope_cos, (size_t)p * HALF + d, cs);
       load8<RV_F32>(a.rope_sin, (size_t)p * HALF + d, sn);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      gq1[j] = a.q_gain ? a.q_gain[d + j] : 0.f;
-      gq2[j] = a.q_gain ? a.q_gain[HALF + d + j] : 0.f;
-      gk1[j] = a.k_gain ? a.k_gain[d + j] : 0.f;
-      gk2[j] = a.k_gain ? a.k_gain[HALF + d + j] : 0.f;
+    if (a.q_gain) {
+      load8<RV_F32>(a.q_gain, d, gq1);
+      load8<RV_F32>(a.q_gain, HALF + d, gq2);
+    }
+    if (a.k_gain) {
+      load8<RV_F32>(a.k_gain, d, gk1);
+      load8<RV_F32>(a.k_gain, HALF + d, gk2);
     }
     for (int h0 = h_lo + tid / per_head; h0 < h_end; h0 += kHeadBatch * par) {
       float y1[kHeadBatch][8], y2[kHeadBatch][8];

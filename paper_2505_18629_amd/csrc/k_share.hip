@@ -21,7 +21,8 @@ enum { KIND_NONE = 0, KIND_FEW = 1, KIND_MANY = 2, KIND_MANY2 = 3 };
 // by queries q_begin.. of nq (query slots of one kv head).
 struct Unit {
   int seq, kbeg, kend, nq, q_begin, slot, kvh;
-  int first, rmax, tiles;  // group: its first member, rows per member; own part: first = -1
+  int first, rmax;  // shared part: the group's first member, rows per member
+  int pos0, row0;   // own part
 };
 
 // Query slot q of a unit: its row, head and the last key it may see.
@@ -32,7 +33,7 @@ struct Query {
 
 template <int PART>
 RV_DEV bool unit_of(const ShareArgs& a, int x, Unit& u) {
-  const SharePart& sp = PART ? a.p.own : a.p.sh;
+  const SharePart& sp = PART ? a.part : a.sh;
   // query groups of one (run, sequence, kv head) are 8 workgroups apart: the
   // same XCD, whose L2 then holds their tiles
   const int j = x / 8, per = j / sp.nqg, qg = j % sp.nqg;
@@ -42,30 +43,28 @@ RV_DEV bool unit_of(const ShareArgs& a, int x, Unit& u) {
   u.kvh = i % a.n_kv;
   i /= a.n_kv;
   const int G = a.n_heads / a.n_kv;
+  u.q_begin = qg * sp.qpw;
   if (PART) {
-    if (i >= a.p.nseq) return false;
-    const int n = a.row0[i + 1] - a.row0[i], g = a.p.group_of[i];
-    const int k0 = g == 255 ? 0 : a.p.tiles[g] * kKB;
+    if (i >= a.nseq) return false;
+    u.pos0 = a.seq[i].pos0;
+    u.row0 = a.seq[i].row0;
+    u.nq = (a.seq[i + 1].row0 - u.row0) * G;
+    const int k0 = a.groups ? a.skip[i] * kKB : 0;
     u.seq = i;
-    u.first = -1;
-    u.rmax = 0;
-    u.nq = n * G;
-    u.q_begin = qg * sp.qpw;
     if (u.q_begin >= u.nq) return false;
     const int q_last = min(u.nq, u.q_begin + sp.qpw) - 1;
     u.kbeg = k0 + run * sp.ks;
-    u.kend = min(a.pos0[i] + q_last / G + 1, u.kbeg + sp.ks);
-    u.slot = (a.p.groups ? a.p.sh.ns : 0) + run;
+    u.kend = min(u.pos0 + q_last / G + 1, u.kbeg + sp.ks);
+    u.slot = (a.groups ? a.sh.ns : 0) + run;
   } else {
-    if (i >= a.p.groups) return false;
-    u.first = a.p.first[i];
-    u.rmax = a.p.rmax[i];
-    u.seq = a.p.member[u.first];
-    u.nq = (a.p.first[i + 1] - u.first) * u.rmax * G;
-    u.q_begin = qg * sp.qpw;
+    if (i >= a.groups) return false;
+    u.first = a.first[i];
+    u.rmax = a.rmax[i];
+    u.seq = a.member[u.first];
+    u.nq = (a.first[i + 1] - u.first) * u.rmax * G;
     if (u.q_begin >= u.nq) return false;
     u.kbeg = run * sp.ks;
-    u.kend = min(a.p.tiles[i] * kKB, u.kbeg + sp.ks);
+    u.kend = min(a.tiles[i] * kKB, u.kbeg + sp.ks);
     u.slot = run;
   }
   return u.kbeg < u.kend;
@@ -79,13 +78,13 @@ RV_DEV Query query_of(const ShareArgs& a, const Unit& u, int q) {
   r.head = u.kvh * G + qc % G;
   if (PART) {
     r.valid = q < u.nq;
-    r.row = a.row0[u.seq] + qc / G;
-    r.last = a.pos0[u.seq] + qc / G;
+    r.row = u.row0 + qc / G;
+    r.last = u.pos0 + qc / G;
   } else {
-    const int i = qc / G, m = i / u.rmax, seq = a.p.member[u.first + m], n = a.row0[seq + 1] - a.row0[seq];
-    const int k = i - m * u.rmax;
+    const int i = qc / G, m = i / u.rmax, seq = a.member[u.first + m];
+    const int row0 = a.seq[seq].row0, n = a.seq[seq + 1].row0 - row0, k = i - m * u.rmax;
     r.valid = q < u.nq && k < n;
-    r.row = a.row0[seq] + min(k, n - 1);
+    r.row = row0 + min(k, n - 1);
     r.last = 0x7fffffff;
   }
   return r;
@@ -94,7 +93,7 @@ RV_DEV Query query_of(const ShareArgs& a, const Unit& u, int q) {
 // The last key that every query of a unit sees.
 template <int PART>
 RV_DEV int first_limit(const ShareArgs& a, const Unit& u) {
-  return PART ? a.pos0[u.seq] + u.q_begin / (a.n_heads / a.n_kv) : 0x7fffffff;
+  return PART ? u.pos0 + u.q_begin / (a.n_heads / a.n_kv) : 0x7fffffff;
 }
 
 // Slot that holds tile t of table row seq, and the tile's first element there in
@@ -155,7 +154,7 @@ RV_DEV void put_out4(const ShareArgs& a, int hd, int row, int head, int d, const
 }
 
 RV_DEV size_t part_index(const ShareArgs& a, int slot, int row, int head) {
-  return ((size_t)slot * a.p.rows + row) * a.n_heads + head;
+  return ((size_t)slot * a.rows + row) * a.n_heads + head;
 }
 
 // Softmax weights of one query's scores of NB 16-key blocks: masks keys past
@@ -596,7 +595,7 @@ RV_DEV void attend_part(const ShareArgs& a, int x, uint16_t (&sm0)[4][kKB * HD],
   else if constexpr (KIND == KIND_MANY2) attend_many<HD, PART, 2, QLO>(a, u, sm0, sm1);
 }
 template <int HD, int SH, int OW, bool QLO>
-__global__ __launch_bounds__(512) void k_share(ShareArgs a) {
+__global__ __launch_bounds__(512, HD <= 64 && (OW == KIND_MANY || OW == KIND_NONE) && SH != KIND_MANY2 ? 4 : 2) void k_share(ShareArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t sm0[4][kKB * HD];
   __shared__ __attribute__((aligned(16))) uint16_t sm1[4][kKB * HD];
   int x = blockIdx.x;
@@ -613,23 +612,28 @@ __global__ __launch_bounds__(512) void k_share(ShareArgs a) {
   attend_part<HD, OW, 1, QLO>(a, x, sm0, sm1);
 }
 
-// As take_out, for four keys of an fp32 cache, where infinities keep their sign.
+// As take_out, for four keys of an fp32 cache, where infinities keep their sign:
+// an infinity that a query sees is added to its output as it is.
 template <int DC>
 RV_DEV void take_out_f32(float (&v)[DC], bool vis, f32x4_t (&o)[DC]) {
   const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
   const float see = vis ? 1.f : 0.f;
 #pragma unroll
   for (int e = 0; e < DC; ++e) {
-    const f32x4_t nan = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e] != v[e] ? 1.f : 0.f, see, zero, 0, 0, 0);
-    const f32x4_t up = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e] == INFINITY ? 1.f : 0.f, see, zero, 0, 0, 0);
-    const f32x4_t down = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e] == -INFINITY ? 1.f : 0.f, see, zero, 0, 0, 0);
+    const uint32_t b = __float_as_uint(v[e]), inf = 0x7f800000u;
+    const bool odd = (b & inf) == inf, is_nan = odd && (b & 0x007fffffu);
+    // counts of what each query sees: 1 for +inf, 2^10 for -inf, 2^20 for NaN (at most 4 keys each)
+    const float mark = !odd ? 0.f : is_nan ? 1048576.f : (int)b < 0 ? 1024.f : 1.f;
+    const f32x4_t seen = __builtin_amdgcn_mfma_f32_16x16x4f32(mark, see, zero, 0, 0, 0);
+    v[e] = odd ? 0.f : v[e];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (up[i] > 0.f) o[e][i] += INFINITY;
-      if (down[i] > 0.f) o[e][i] -= INFINITY;
-      if (nan[i] > 0.f) o[e][i] = __builtin_nanf("");
+      const int n = (int)seen[i];
+      float add = n & 1023 ? INFINITY : 0.f;
+      add -= (n >> 10) & 1023 ? INFINITY : 0.f;
+      add += n >> 20 ? __builtin_nanf("") : 0.f;
+      o[e][i] += add;
     }
-    if (!__builtin_isfinite(v[e])) v[e] = 0.f;
   }
 }
 
@@ -638,13 +642,13 @@ RV_DEV void take_out_f32(float (&v)[DC], bool vis, f32x4_t (&o)[DC]) {
 // straight from the row-major cache.  The k slots of an MFMA may hold any four
 // dims that both operands agree on, so a lane's 16-byte load of dims
 // 16c + 4(l/16) .. +3 feeds four MFMAs, and P comes straight from the scores.
+// Bound by latency: all loads of KT keys, K and V, are issued together.
 template <int HD, int PART>
-__global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
-  constexpr int DC = HD / 16;
-  Unit u;
-  if (!unit_of<PART>(a, blockIdx.x, u)) return;
+RV_DEV void attend_f32(const ShareArgs& a, const Unit& u) {
+  constexpr int DC = HD / 16, KT = HD == 128 ? 32 : 64, NB = KT / 16;
   const int lane = threadIdx.x, g = lane >> 4, c16 = lane & 15;
   const Query q = query_of<PART>(a, u, u.q_begin + c16);
+  const int first_last = first_limit<PART>(a, u);
   f32x4_t qv[DC];
 #pragma unroll
   for (int c = 0; c < DC; ++c) {
@@ -664,56 +668,73 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
 #pragma unroll
   for (int t = 0; t < DC; ++t) o[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  const int first_last = first_limit<PART>(a, u);
 
-  for (int k0 = u.kbeg; k0 < u.kend; k0 += kKB) {
-    const size_t base = tile_base<HD>(a, u.seq, u.kvh, k0 / kKB);
+  for (int k0 = u.kbeg; k0 < u.kend; k0 += KT) {
+    const size_t base = tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + (size_t)(k0 % kKB) * HD;
     const float* kb = (const float*)a.kc + base;
     const float* vb = (const float*)a.vc + base;
-    f32x4_t s[4];
+    f32x4_t kv[NB][DC];
+    float v[NB][4][DC];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      const float* kr = kb + (16 * t + c16) * HD + 4 * g;
-      f32x4_t kv[DC];
+    for (int t = 0; t < NB; ++t)
 #pragma unroll
-      for (int c = 0; c < DC; ++c) kv[c] = *(const f32x4_t*)(kr + 16 * c);
+      for (int c = 0; c < DC; ++c) kv[t][c] = *(const f32x4_t*)(kb + (16 * t + c16) * HD + 4 * g + 16 * c);
 #pragma unroll
-      for (int c = 0; c < DC; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[c][i], qv[c][i], s[t], 0, 0, 0);
-    }
-    const bool masked = k0 + kKB > u.kend || k0 + kKB - 1 > first_last;
-    float rescale;
-    if (softmax_step<4>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l, &rescale)) {
-#pragma unroll
-      for (int t = 0; t < DC; ++t) o[t] *= rescale;
-    }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < NB; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int kk = 16 * t + 4 * g + i;
-        const float* vr = vb + kk * HD + c16 * DC;
-        float v[DC];
+        const float* vr = vb + (16 * t + 4 * g + i) * HD + c16 * DC;
         if constexpr (DC == 2) {
           const float2 x = *(const float2*)vr;
-          v[0] = x.x;
-          v[1] = x.y;
+          v[t][i][0] = x.x;
+          v[t][i][1] = x.y;
         } else {
 #pragma unroll
           for (int e = 0; e < DC; e += 4) {
             const f32x4_t x = *(const f32x4_t*)(vr + e);
 #pragma unroll
-            for (int f = 0; f < 4; ++f) v[e + f] = x[f];
+            for (int f = 0; f < 4; ++f) v[t][i][e + f] = x[f];
           }
         }
-        bool bad = false;
+      }
+    f32x4_t s[NB];
 #pragma unroll
-        for (int e = 0; e < DC; ++e) bad |= !__builtin_isfinite(v[e]);
-        if (masked && __any(bad)) take_out_f32<DC>(v, k0 + kk < u.kend && k0 + kk <= q.last, o);
+    for (int t = 0; t < NB; ++t) s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // the key blocks side by side: dependent MFMAs are NB apart
 #pragma unroll
-        for (int e = 0; e < DC; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[e], s[t][i], o[e], 0, 0, 0);
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[t][c][i], qv[c][i], s[t], 0, 0, 0);
+    const bool masked = k0 + KT > u.kend || k0 + KT - 1 > first_last;
+    float rescale;
+    if (softmax_step<NB>(s, k0, u.kend, q.last, g, a.scale_log2, masked, m, l, &rescale)) {
+#pragma unroll
+      for (int t = 0; t < DC; ++t) o[t] *= rescale;
+    }
+    bool bad = false;
+    if (masked) {
+      uint32_t bits = 0;  // bit 31: an exponent of all ones
+#pragma unroll
+      for (int t = 0; t < NB; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < DC; ++e) bits |= (__float_as_uint(v[t][i][e]) & 0x7f800000u) + 0x00800000u;
+      bad = __any((int)bits < 0);
+    }
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (bad) {
+          const int key = k0 + 16 * t + 4 * g + i;
+          take_out_f32<DC>(v[t][i], key < u.kend && key <= q.last, o);
+        }
+#pragma unroll
+        for (int e = 0; e < DC; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i][e], s[t][i], o[e], 0, 0, 0);
       }
   }
   l = rows4_sum(l);
@@ -734,6 +755,16 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
     a.part_ml[2 * e + 1] = l;
   }
 }
+template <int HD>
+__global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
+  const int x = blockIdx.x, n = a.runs_sh * 8;
+  Unit u;
+  if (x < n) {
+    if (unit_of<0>(a, x, u)) attend_f32<HD, 0>(a, u);
+  } else if (unit_of<1>(a, x - n, u)) {
+    attend_f32<HD, 1>(a, u);
+  }
+}
 
 // ----------------------------------------------------------- merge
 // hd / 4 lanes per (row, head): one pass over the runs that had keys for the
@@ -741,15 +772,15 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_share_merge(ShareArgs a) {
   constexpr int LPQ = HD / 4, BATCH = 8;
-  const int b = blockIdx.y, n = a.row0[b + 1] - a.row0[b];
+  const int b = blockIdx.y, row0 = a.seq[b].row0, n = a.seq[b + 1].row0 - row0;
   const int i = blockIdx.x * (256 / LPQ) + threadIdx.x / LPQ, d = threadIdx.x % LPQ * 4;
   if (i >= n * a.n_heads) return;
-  const int r = i / a.n_heads, head = i % a.n_heads, row = a.row0[b] + r;
-  const int g = a.p.group_of[b], k0 = g == 255 ? 0 : a.p.tiles[g] * kKB;
-  const int n_sh = g == 255 ? 0 : (k0 + a.p.sh.ks - 1) / a.p.sh.ks;
-  const int n_own = (a.pos0[b] + r - k0) / a.p.own.ks + 1;
-  const int skip = (a.p.groups ? a.p.sh.ns : 0) - n_sh;  // slots of shared runs that this row has not
-  const size_t e0 = part_index(a, 0, row, head), stride = (size_t)a.p.rows * a.n_heads;
+  const int r = i / a.n_heads, head = i % a.n_heads, row = row0 + r;
+  const int k0 = a.groups ? a.skip[b] * kKB : 0;
+  const int n_sh = k0 ? (k0 + a.sh.ks - 1) / a.sh.ks : 0;
+  const int n_own = (a.seq[b].pos0 + r - k0) / a.part.ks + 1;
+  const int skip = (a.groups ? a.sh.ns : 0) - n_sh;  // slots of shared runs that this row has not
+  const size_t e0 = part_index(a, 0, row, head), stride = (size_t)a.rows * a.n_heads;
   float M = -INFINITY, L = 0.f;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < n_sh + n_own; s0 += BATCH) {
@@ -780,12 +811,6 @@ __global__ __launch_bounds__(256) void k_share_merge(ShareArgs a) {
   put_out4<DT>(a, HD, row, head, d, acc * (1.0f / L));
 }
 
-template <int HD, int PART>
-hipError_t launch_f32(const ShareArgs& a, int runs, hipStream_t st) {
-  if (runs) k_share_f32<HD, PART><<<(unsigned)runs * 8, 64, 0, st>>>(a);
-  return hipGetLastError();
-}
-
 template <int HD, int SH, int OW>
 void launch_kinds(const ShareArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)(a.runs_sh + a.runs_own) * 8;
@@ -800,18 +825,18 @@ size_t part_runs(const SharePart& p, int n, int n_kv) { return ((size_t)p.ns * n
 
 template <int HD>
 hipError_t launch_all(int dtype, ShareArgs& a, hipStream_t st) {
-  a.direct = a.p.groups == 0 && a.p.own.ns == 1;
-  const size_t sh = a.p.groups ? part_runs(a.p.sh, a.p.groups, a.n_kv) : 0, own = part_runs(a.p.own, a.p.nseq, a.n_kv);
+  a.direct = a.groups == 0 && a.part.ns == 1;
+  const size_t sh = a.groups ? part_runs(a.sh, a.groups, a.n_kv) : 0, own = part_runs(a.part, a.nseq, a.n_kv);
   if ((sh + own) * 8 > 0x7fffffff) return hipErrorInvalidValue;
   a.runs_sh = (int)sh;
   a.runs_own = (int)own;
-  a.lead_sh = a.p.own_last ? a.runs_sh : std::min(a.runs_sh, 16);
-  a.lead_own = a.p.own_last ? 0 : a.runs_own / 2;
+  a.lead_sh = a.own_last ? a.runs_sh : std::min(a.runs_sh, 16);
+  a.lead_own = a.own_last ? 0 : a.runs_own / 2;
   if (dtype == RV_F32) {
-    if (hipError_t e = launch_f32<HD, 0>(a, a.runs_sh, st); e != hipSuccess) return e;
-    if (hipError_t e = launch_f32<HD, 1>(a, a.runs_own, st); e != hipSuccess) return e;
+    k_share_f32<HD><<<(unsigned)(a.runs_sh + a.runs_own) * 8, 64, 0, st>>>(a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   } else {
-    const int kinds = (sh ? kind_of(a.p.sh) : KIND_NONE) * 4 + kind_of(a.p.own);
+    const int kinds = (sh ? kind_of(a.sh) : KIND_NONE) * 4 + kind_of(a.part);
     switch (kinds) {
       case KIND_NONE * 4 + KIND_FEW: launch_kinds<HD, KIND_NONE, KIND_FEW>(a, st); break;
       case KIND_FEW * 4 + KIND_FEW: launch_kinds<HD, KIND_FEW, KIND_FEW>(a, st); break;
@@ -828,9 +853,9 @@ hipError_t launch_all(int dtype, ShareArgs& a, hipStream_t st) {
   }
   if (a.direct) return hipSuccess;
   int longest = 0;
-  for (int b = 0; b < a.p.nseq; ++b) longest = std::max(longest, a.row0[b + 1] - a.row0[b]);
+  for (int b = 0; b < a.nseq; ++b) longest = std::max(longest, a.seq[b + 1].row0 - a.seq[b].row0);
   constexpr int per = 256 / (HD / 4);
-  const dim3 grid((unsigned)(((size_t)longest * a.n_heads + per - 1) / per), a.p.nseq);
+  const dim3 grid((unsigned)(((size_t)longest * a.n_heads + per - 1) / per), a.nseq);
   if (dtype == RV_BF16) k_share_merge<RV_BF16, HD><<<grid, 256, 0, st>>>(a);
   else k_share_merge<RV_F32, HD><<<grid, 256, 0, st>>>(a);
   return hipGetLastError();

@@ -127,9 +127,25 @@ void plan_attend(const rv_cache* c, const int* pos0, const int* row0, ShareArgs&
   a.n_kv = mc.n_kv_heads;
   a.kv_len = c->kv_len;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)mc.head_dim));
-  std::copy(pos0, pos0 + c->B, a.pos0);
-  std::copy(row0, row0 + c->B + 1, a.row0);
-  plan_share(c->tiles, mc.dtype == RV_BF16, pos0, row0, mc.n_heads, mc.n_kv_heads, mc.head_dim, c->part_entries, a.p);
+  SharePlan p;
+  plan_share(c->tiles, mc.dtype == RV_BF16, pos0, row0, mc.n_heads, mc.n_kv_heads, mc.head_dim, c->part_entries, p);
+  a.nseq = p.nseq;
+  a.rows = p.rows;
+  a.groups = p.groups;
+  a.sh = p.sh;
+  a.part = p.own;
+  a.own_last = p.own_last;
+  for (int b = 0; b < c->B; ++b) {
+    a.seq[b] = ShareSeq{pos0[b], row0[b]};
+    a.skip[b] = p.group_of[b] == 255 ? 0 : (uint16_t)p.tiles[p.group_of[b]];
+  }
+  a.seq[c->B].row0 = row0[c->B];
+  if (p.groups) {
+    std::copy(p.member, p.member + c->B, a.member);
+    std::copy(p.first, p.first + p.groups + 1, a.first);
+    std::copy(p.tiles, p.tiles + p.groups, a.tiles);
+    std::copy(p.rmax, p.rmax + p.groups, a.rmax);
+  }
 }
 
 extern "C" {
@@ -174,6 +190,8 @@ rv_status rv_cache_append(rv_cache* c, int32_t layer, int32_t batch, const int32
     if (rv_status s = check_rows("q", rows->d_q, rows->ld_q, rows->q_width, qd, io); s != RV_OK) return s;
     if (rv_status s = check_rows("q output", rows->d_q_out, rows->ld_q_out, rows->q_width, qd, io); s != RV_OK) return s;
   }
+  if (((uintptr_t)rows->d_q_gain | (uintptr_t)rows->d_k_gain) & 15)
+    return rv_fail(RV_E_ARG, "gains must start at multiples of 16 bytes");
   const Planes p = layer_planes(c, layer);
   a.q = rows->d_q;
   a.k = rows->d_k;

@@ -292,6 +292,9 @@ hipError_t launch_own(const OwnArgs& a, int n, hipStream_t st);
 
 // Attention over a cache whose sequences may share tiles (rv_tiles.h: SharePlan).
 enum { ROWS_OPERAND = 2 };  // q / out as operand planes; else rows of RV_F32 or RV_BF16
+struct ShareSeq {
+  int pos0, row0;        // position of the sequence's first row, and that row
+};
 struct ShareArgs {
   const void *q, *q2;    // rows [rows][ldq], or operand planes
   void *out, *out2;
@@ -302,11 +305,21 @@ struct ShareArgs {
   int q_kind, o_kind;
   int n_heads, n_kv, kv_len;
   float scale_log2;
+  int nseq, rows, groups;
+  SharePart sh, part;    // the shared and the own part (rv_tiles.h)
+  int own_last;          // the own part fits beside the shared part's last round
   int direct;            // one run and no groups: the output is final (this and the next are the launcher's)
   int runs_sh, runs_own;  // workgroups of the two parts, in runs of 8
   int lead_sh, lead_own;  // how many of each start first
-  int pos0[RV_MAX_BATCH], row0[RV_MAX_BATCH + 1];
-  SharePlan p;
+  // What follows lies in other cache lines of the kernel arguments, which live in
+  // host memory: a workgroup reads one pair of records, and the rest only where
+  // tiles are shared (one decode step of one sequence, 128 workgroups, 8.3 us
+  // with separate arrays).
+  ShareSeq seq[RV_MAX_BATCH + 1];
+  uint16_t skip[RV_MAX_BATCH];  // tiles that the sequence's group attends for it
+  uint8_t member[RV_MAX_BATCH];
+  int16_t first[kShareGroups + 1];
+  int32_t tiles[kShareGroups], rmax[kShareGroups];
 };
 static_assert(sizeof(ShareArgs) <= 4096, "kernel arguments");
 // Every launch of one call: shared part, own part, merge.

@@ -297,7 +297,7 @@ constexpr int kCuts = sizeof kCutCounts / sizeof kCutCounts[0];
 inline double share_wg_us(bool bf16, int qpw, int keys, int hd) {
   const double f = hd / 128.0;
   if (!bf16) return 2.5 + (keys + kTile - 1) / kTile * 1.5 * f;      // a wave of 16 queries
-  if (qpw == 16) return 4.0 + keys * 8.0 * hd / 4.5e4;               // what one CU draws
+  if (qpw == 16) return 4.0 + keys * 8.0 * hd / 3.0e4;               // what one CU draws
   return 5.0 + (keys + kTile - 1) / kTile * (qpw == 128 ? 3.2 : 5.2) * f;
 }
 
@@ -326,7 +326,7 @@ inline int cut_part(bool bf16, const ShareUnit* u, int n, int n_kv, int hd, int 
 
 // Launch shape of a call.  part_entries: (run, row, head) results that the
 // partial buffer holds; n_heads * rows <= part_entries / 2 always fits.  Both
-// parts run in one launch (fp32 caches: two).  The shared part's workgroups are
+// parts run in one launch.  The shared part's workgroups are
 // the long ones: they take whole rounds of the CUs, the own part's fill what
 // those leave and then add their share and half of one; every run costs its
 // results' write and the merge's read.  (64 continuations of 32768 keys at the

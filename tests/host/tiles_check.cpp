@@ -346,6 +346,7 @@ static void refusals() {
   CHECK((r = ok, r.ld_q_out = 127, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.n_rows = 2, append(r)) == RV_E_ARG && (r = ok, r.q_width = 96, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.kv_width = 28, append(r)) == RV_E_ARG);
+  CHECK((r = ok, r.d_k_gain = (const float*)(mem + 4), append(r)) == RV_E_ARG);
   CHECK(rv_cache_append(c, 0, 3, pos, n, &ok, nullptr) == RV_E_ARG);
   auto read = [&](int64_t rows, int io = RV_F32, void* v = mem, int w = 32, int batch = 4) {
     return rv_cache_read(c, 0, batch, pos, n, io, rows, w, mem, 32, v, 32, nullptr);
