@@ -7,15 +7,18 @@ namespace {
 constexpr int kBlockPos = 32;  // positions per workgroup of append and read: one V block of a bf16 cache
 
 // Workgroup x of a launch over the 32-position blocks of every sequence's rows:
-// sequence b with blk0[b] <= x < blk0[b + 1].
+// sequence b with blk0[b] <= x < blk0[b + 1].  The lanes look at all entries at
+// once: kernel arguments come from host memory, and a search would wait for one
+// after the other.
 RV_DEV int find_seq(const int* blk0, int B, int x) {
-  int lo = 0, hi = B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (blk0[mid] <= x) lo = mid;
-    else hi = mid - 1;
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < RV_MAX_BATCH / 64; ++j) {
+    const int b = lane + 64 * j;
+    if (64 * j < B) n += __popcll(__ballot(b < B && blk0[b] <= x));
   }
-  return lo;
+  return n - 1;
 }
 
 // 8 consecutive values of a row of fp32 or bf16 as fp32, and back.
@@ -86,13 +89,12 @@ RV_DEV bool group_touched(int g, int k_lo, int k_hi) {
 // d+hd/2..: 16-byte loads and stores throughout, the norm is a sum over those
 // threads, and rows are adjacent in a wave, so that a K unit of the bf16 cache
 // (16 positions x 32 dims) is written whole.  A thread keeps its row's rotary
-// factors for kHeadBatch heads whose loads it issues together (one head per
-// workgroup reads as many bytes of factors as of rows: 38 us for 4.1k ragged
-// rows of 32/8 heads x 128 in bf16).  A V unit holds 8 positions of one dim:
+// factors for up to kHeadRounds rounds of kHeadBatch heads whose loads it issues
+// together.  A V unit holds 8 positions of one dim:
 // rows go through LDS and each thread writes the 8 positions of a (dim, slot
 // group) with one store -- 2-byte stores of single positions remain for the
 // groups that the rows fill in part.
-constexpr int kHeadBatch = 4;
+constexpr int kHeadBatch = 2, kHeadRounds = 4;
 template <int DT, int IO, int HD>
 __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   constexpr int HALF = HD / 2, TPH = HD / 16;  // threads per (row, head)
@@ -391,7 +393,7 @@ int span_blocks(int pos, int rows) { return rows ? (pos + rows - 1) / kBlockPos 
 hipError_t launch_append(int dtype, int io, int hd, int max_rows, AppendArgs& a, hipStream_t st) {
   // heads side by side, and as many rounds of them as leave four workgroups to a CU
   const int heads = a.n_heads + a.n_kv, par = heads_per_wg(max_rows, hd / 16, heads);
-  int rounds = kHeadBatch;
+  int rounds = kHeadRounds;
   while (rounds > 1 && (long long)a.blk0[a.B] * ((heads + par * rounds - 1) / (par * rounds)) < 1024) rounds /= 2;
   a.hpw = par * rounds;
   a.qk_groups = (heads + a.hpw - 1) / a.hpw;

@@ -292,13 +292,18 @@ struct ShareCut {
 constexpr int kCutCounts[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80};
 constexpr int kCuts = sizeof kCutCounts / sizeof kCutCounts[0];
 
+// The own part's workgroups take this much longer beside the shared part's (64
+// continuations of 32768 keys, about 1000 own keys each: 160 workgroups of the
+// shared part leave the other CUs enough time, 253 us; 192 do not, 296).
+constexpr double kBeside = 1.35;
+
 // us of a workgroup that attends `keys` keys: prologue, epilogue and latencies,
 // then the keys at its rate (head_dim 128; others in proportion).
 inline double share_wg_us(bool bf16, int qpw, int keys, int hd) {
   const double f = hd / 128.0;
   if (!bf16) return 2.5 + (keys + kTile - 1) / kTile * 1.5 * f;      // a wave of 16 queries
-  if (qpw == 16) return 4.0 + keys * 8.0 * hd / 3.0e4;               // what one CU draws
-  return 5.0 + (keys + kTile - 1) / kTile * (qpw == 128 ? 3.2 : 5.2) * f;
+  if (qpw == 16) return 4.0 + keys * 8.0 * hd / 4.0e4;               // what one CU draws
+  return 5.0 + (keys + kTile - 1) / kTile * (qpw == 128 ? 2.6 : 5.3) * f;
 }
 
 // The cuts of a part worth trying, within max_ns runs; their number.
@@ -372,9 +377,10 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
       const int runs = a[i].ns + c[j].ns;
       if (runs > fit && (i || j)) continue;
       const double rounds = std::ceil(a[i].wgs / slots), gap = rounds * slots * a[i].longest - a[i].sum;
+      const double beside = c[j].sum * kBeside;
       double t = rounds * a[i].longest;
       if (!rounds) t = c[j].wgs <= slots ? c[j].longest : c[j].sum / slots + c[j].longest / 2;
-      else if (c[j].sum > gap) t += (c[j].sum - gap) / slots + c[j].longest / 2;
+      else if (beside > gap) t += (beside - gap) / slots + c[j].longest / 2;
       t = std::max(std::max(t, c[j].longest), stream);
       if (runs > 1) t += 5.0 + 0.1 * runs + (double)runs * p.rows * n_heads * hd * 8 / 3.5e6;
       if ((!i && !j) || t < best) {
@@ -383,7 +389,7 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
         p.sh.ns = a[i].ns;
         p.own.ks = c[j].ks;
         p.own.ns = c[j].ns;
-        p.own_last = c[j].sum <= gap;
+        p.own_last = beside <= gap;
       }
     }
 }
