@@ -275,7 +275,8 @@ rv_status rv_cache_dims(const rv_cache* c, int32_t* h_dims);
 rv_status rv_cache_append(rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
                           const rv_rows* rows, void* stream);
 
-/* Reads K and V rows of one layer back as values (hi + lo for bf16 models). */
+/* Reads K and V rows of one layer back as values (hi + lo for bf16 models, where
+ * an infinity, whose lo part is inf - inf, comes back as NaN). */
 rv_status rv_cache_read(const rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
                         int32_t dtype, int64_t n_rows, int64_t width, void* d_k, int64_t ld_k, void* d_v, int64_t ld_v,
                         void* stream);
@@ -313,9 +314,10 @@ rv_status rv_cache_attend(const rv_cache* c, int32_t layer, int32_t batch, const
 
 /* From now on the passes of this model normalise queries and keys for each head
  * before the rotation (as rv_cache_append does), with gains [n_layers][head_dim]
- * fp32 in the caller's device memory (at multiples of 16 bytes, kept for as long
- * as the model runs); NULL for both: no norms, as after rv_init_weights. */
-rv_status rv_model_qk_norm(rv_model* m, const float* d_q_gain, const float* d_k_gain);
+ * fp32 in the caller's device memory (`count` = n_layers * head_dim values each,
+ * at multiples of 16 bytes, kept for as long as the model runs); NULL for both: no
+ * norms, as after rv_init_weights. */
+rv_status rv_model_qk_norm(rv_model* m, const float* d_q_gain, const float* d_k_gain, int64_t count);
 
 /* ---- inspection (tests and benchmarks) ---- */
 

@@ -106,7 +106,7 @@ _sig = {
     "rv_cache_fork": ([_vp, _i32, _i32, _i32, _cp, _vp], ctypes.c_int),
     "rv_cache_attend": ([_vp, _i32, _i32, _cp, _cp, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp], ctypes.c_int),
     "rv_cache_dims": ([_vp, _vp], ctypes.c_int),
-    "rv_model_qk_norm": ([_vp, _vp, _vp], ctypes.c_int),
+    "rv_model_qk_norm": ([_vp, _vp, _vp, _i64], ctypes.c_int),
     "rv_debug_cache_span": ([_vp, _i32, ctypes.POINTER(_sz), ctypes.POINTER(_sz)], ctypes.c_int),
     "rv_debug_fuse_accept": ([_vp, _vp, _P_i32, _vp, _i32, ctypes.POINTER(rv_fusion), _vp, _vp, _vp], ctypes.c_int),
     "rv_debug_output": ([_vp, _i32, _vp, _sz, _vp], ctypes.c_int),
@@ -374,7 +374,11 @@ def rv_cache_attend(cache: int, layer: int, positions, counts, q, out, stream=No
 
 def rv_model_qk_norm(model: int, q_gain, k_gain) -> None:
     """q_gain, k_gain: device float32 [n_layers][head_dim], kept by the caller; None for both: no norms."""
-    _check(_lib.rv_model_qk_norm(model, _dev(q_gain), _dev(k_gain)))
+    for t in (q_gain, k_gain):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or q_gain is None or
+                              t.shape != q_gain.shape):
+            raise ValueError("gains must be contiguous float32 of one shape")
+    _check(_lib.rv_model_qk_norm(model, _dev(q_gain), _dev(k_gain), 0 if q_gain is None else q_gain.numel()))
 
 
 def rv_debug_cache_span(cache: int, which: int):

@@ -15,7 +15,7 @@ namespace {
 constexpr int kKB = kTile;
 
 // How a part is computed (kinds of rv_tiles.h): by k_share's workgroups of 512.
-enum { KIND_NONE = 0, KIND_FEW = 1, KIND_MANY = 2, KIND_MANY2 = 3 };
+enum { KIND_NONE = 0, KIND_FEW = 1, KIND_MANY = 2, KIND_MANY2 = 3, KIND_STREAM = 4 };
 
 // What one workgroup attends: keys [kbeg, kend) as table row `seq` reads them,
 // by queries q_begin.. of nq (query slots of one kv head).
@@ -446,10 +446,12 @@ RV_DEV void attend_many(const ShareArgs& a, const Unit& u, uint16_t (&sm0)[4][kK
 // ----------------------------------------------------------- bf16, at most 16 queries
 // Decode steps: the 8 waves share the 16 queries and split the keys, wave w
 // taking tiles w, w + 8, ... of KT keys straight to registers; their states
-// merge in LDS.
+// merge in LDS.  STREAM: nontemporal loads, for calls whose keys exceed the
+// last-level cache anyway (64 sequences of 1000 keys, 524 MB: 110 -> 98 us at the
+// 70B shape, 101 -> 91 at 8B; with 112 MB, 33.2 -> 34.8).
 // red: 8 x 16 x HD values in LDS, 16-byte columns xor-ed with the query so that
 // the 16 queries of a column lie in different banks; red_ml: 2 x 8 x 16.
-template <int HD, int PART, bool QLO>
+template <int HD, int PART, bool QLO, bool STREAM>
 RV_DEV void attend_few(const ShareArgs& a, const Unit& u, float* red, float* red_ml) {
   constexpr int KT = HD == 128 ? 32 : 64, NW = 8, NB = KT / 16, NC = KT / 32, DC = HD / 32, DT = HD / 16;
   constexpr int COLS = HD / 4 < 16 ? HD / 4 : 16;  // columns that the xor permutes
@@ -470,6 +472,9 @@ RV_DEV void attend_few(const ShareArgs& a, const Unit& u, float* red, float* red
   // (uniform offsets: the loads then need one lane offset and no 64-bit addresses)
   auto at = [&](int k0) { return tile_base<HD>(a, u.seq, u.kvh, k0 / kKB) + (size_t)(k0 % kKB) * HD; };
   const unsigned lane16 = lane * 16;
+  auto load = [](const char* p) {
+    return STREAM ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p;
+  };
   auto load_k = [&](size_t o) {
 #pragma unroll
     for (int pl = 0; pl < 2; ++pl)
@@ -477,7 +482,7 @@ RV_DEV void attend_few(const ShareArgs& a, const Unit& u, float* red, float* red
       for (int t = 0; t < NB; ++t)
 #pragma unroll
         for (int c = 0; c < DC; ++c)
-          k[pl][t][c] = *(const u32x4*)((const char*)((const uint16_t*)(pl ? a.kc2 : a.kc) + o + (t * DC + c) * 512) + lane16);
+          k[pl][t][c] = load((const char*)((const uint16_t*)(pl ? a.kc2 : a.kc) + o + (t * DC + c) * 512) + lane16);
   };
   auto load_v = [&](size_t o) {
 #pragma unroll
@@ -486,7 +491,7 @@ RV_DEV void attend_few(const ShareArgs& a, const Unit& u, float* red, float* red
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          v[pl][c][d] = *(const u32x4*)((const char*)((const uint16_t*)(pl ? a.vc2 : a.vc) + o + (c * DT + d) * 512) + lane16);
+          v[pl][c][d] = load((const char*)((const uint16_t*)(pl ? a.vc2 : a.vc) + o + (c * DT + d) * 512) + lane16);
   };
   int k0 = u.kbeg + w * KT;
   size_t next = at(min(k0, last_tile));
@@ -590,7 +595,8 @@ template <int HD, int KIND, int PART, bool QLO>
 RV_DEV void attend_part(const ShareArgs& a, int x, uint16_t (&sm0)[4][kKB * HD], uint16_t (&sm1)[4][kKB * HD]) {
   Unit u;
   if (!unit_of<PART>(a, x, u)) return;
-  if constexpr (KIND == KIND_FEW) attend_few<HD, PART, QLO>(a, u, (float*)&sm0[0][0], (float*)&sm1[0][0]);
+  if constexpr (KIND == KIND_FEW || KIND == KIND_STREAM)
+    attend_few<HD, PART, QLO, KIND == KIND_STREAM>(a, u, (float*)&sm0[0][0], (float*)&sm1[0][0]);
   else if constexpr (KIND == KIND_MANY) attend_many<HD, PART, 1, QLO>(a, u, sm0, sm1);
   else if constexpr (KIND == KIND_MANY2) attend_many<HD, PART, 2, QLO>(a, u, sm0, sm1);
 }
@@ -767,15 +773,20 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
 }
 
 // ----------------------------------------------------------- merge
-// hd / 4 lanes per (row, head): one pass over the runs that had keys for the
-// row, shared runs first, in batches whose loads are issued together.
+// hd / 4 lanes per (row, head), a workgroup per row and 1024 / hd heads: one pass
+// over the runs that had keys for the row, shared runs first, in batches whose
+// loads are issued together.
 template <int DT, int HD>
-__global__ __launch_bounds__(256) void k_share_merge(ShareArgs a) {
+__global__ __launch_bounds__(256) void k_share_merge(ShareArgs a, int head_groups) {
   constexpr int LPQ = HD / 4, BATCH = 8;
-  const int b = blockIdx.y, row0 = a.seq[b].row0, n = a.seq[b + 1].row0 - row0;
-  const int i = blockIdx.x * (256 / LPQ) + threadIdx.x / LPQ, d = threadIdx.x % LPQ * 4;
-  if (i >= n * a.n_heads) return;
-  const int r = i / a.n_heads, head = i % a.n_heads, row = row0 + r;
+  const int row = blockIdx.x / head_groups, lane = threadIdx.x & 63;
+  int b = -1;  // the last sequence that starts at the row or before
+#pragma unroll
+  for (int j = 0; j < RV_MAX_BATCH / 64; ++j)
+    if (64 * j < a.nseq) b += __popcll(__ballot(lane + 64 * j < a.nseq && a.seq[lane + 64 * j].row0 <= row));
+  const int head = blockIdx.x % head_groups * (256 / LPQ) + threadIdx.x / LPQ, d = threadIdx.x % LPQ * 4;
+  if (head >= a.n_heads) return;
+  const int r = row - a.seq[b].row0;
   const int k0 = a.groups ? a.skip[b] * kKB : 0;
   const int n_sh = k0 ? (k0 + a.sh.ks - 1) / a.sh.ks : 0;
   const int n_own = (a.seq[b].pos0 + r - k0) / a.part.ks + 1;
@@ -836,28 +847,29 @@ hipError_t launch_all(int dtype, ShareArgs& a, hipStream_t st) {
     k_share_f32<HD><<<(unsigned)(a.runs_sh + a.runs_own) * 8, 64, 0, st>>>(a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   } else {
-    const int kinds = (sh ? kind_of(a.sh) : KIND_NONE) * 4 + kind_of(a.part);
+    const int kinds = a.stream ? KIND_NONE * 8 + KIND_STREAM : (sh ? kind_of(a.sh) : KIND_NONE) * 8 + kind_of(a.part);
     switch (kinds) {
-      case KIND_NONE * 4 + KIND_FEW: launch_kinds<HD, KIND_NONE, KIND_FEW>(a, st); break;
-      case KIND_FEW * 4 + KIND_FEW: launch_kinds<HD, KIND_FEW, KIND_FEW>(a, st); break;
-      case KIND_MANY * 4 + KIND_FEW: launch_kinds<HD, KIND_MANY, KIND_FEW>(a, st); break;
-      case KIND_MANY2 * 4 + KIND_FEW: launch_kinds<HD, KIND_MANY2, KIND_FEW>(a, st); break;
-      case KIND_NONE * 4 + KIND_MANY: launch_kinds<HD, KIND_NONE, KIND_MANY>(a, st); break;
-      case KIND_MANY * 4 + KIND_MANY: launch_kinds<HD, KIND_MANY, KIND_MANY>(a, st); break;
-      case KIND_MANY2 * 4 + KIND_MANY: launch_kinds<HD, KIND_MANY2, KIND_MANY>(a, st); break;
-      case KIND_NONE * 4 + KIND_MANY2: launch_kinds<HD, KIND_NONE, KIND_MANY2>(a, st); break;
-      case KIND_MANY2 * 4 + KIND_MANY2: launch_kinds<HD, KIND_MANY2, KIND_MANY2>(a, st); break;
+      case KIND_NONE * 8 + KIND_FEW: launch_kinds<HD, KIND_NONE, KIND_FEW>(a, st); break;
+      case KIND_NONE * 8 + KIND_STREAM: launch_kinds<HD, KIND_NONE, KIND_STREAM>(a, st); break;
+      case KIND_FEW * 8 + KIND_FEW: launch_kinds<HD, KIND_FEW, KIND_FEW>(a, st); break;
+      case KIND_MANY * 8 + KIND_FEW: launch_kinds<HD, KIND_MANY, KIND_FEW>(a, st); break;
+      case KIND_MANY2 * 8 + KIND_FEW: launch_kinds<HD, KIND_MANY2, KIND_FEW>(a, st); break;
+      case KIND_NONE * 8 + KIND_MANY: launch_kinds<HD, KIND_NONE, KIND_MANY>(a, st); break;
+      case KIND_MANY * 8 + KIND_MANY: launch_kinds<HD, KIND_MANY, KIND_MANY>(a, st); break;
+      case KIND_MANY2 * 8 + KIND_MANY: launch_kinds<HD, KIND_MANY2, KIND_MANY>(a, st); break;
+      case KIND_NONE * 8 + KIND_MANY2: launch_kinds<HD, KIND_NONE, KIND_MANY2>(a, st); break;
+      case KIND_MANY2 * 8 + KIND_MANY2: launch_kinds<HD, KIND_MANY2, KIND_MANY2>(a, st); break;
       default: return hipErrorInvalidValue;
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (a.direct) return hipSuccess;
-  int longest = 0;
-  for (int b = 0; b < a.nseq; ++b) longest = std::max(longest, a.seq[b + 1].row0 - a.seq[b].row0);
   constexpr int per = 256 / (HD / 4);
-  const dim3 grid((unsigned)(((size_t)longest * a.n_heads + per - 1) / per), a.nseq);
-  if (dtype == RV_BF16) k_share_merge<RV_BF16, HD><<<grid, 256, 0, st>>>(a);
-  else k_share_merge<RV_F32, HD><<<grid, 256, 0, st>>>(a);
+  const int head_groups = (a.n_heads + per - 1) / per;
+  if ((size_t)a.rows * head_groups > 0x7fffffff) return hipErrorInvalidValue;
+  const unsigned grid = (unsigned)a.rows * head_groups;
+  if (dtype == RV_BF16) k_share_merge<RV_BF16, HD><<<grid, 256, 0, st>>>(a, head_groups);
+  else k_share_merge<RV_F32, HD><<<grid, 256, 0, st>>>(a, head_groups);
   return hipGetLastError();
 }
 

@@ -135,6 +135,7 @@ void plan_attend(const rv_cache* c, const int* pos0, const int* row0, ShareArgs&
   a.sh = p.sh;
   a.part = p.own;
   a.own_last = p.own_last;
+  a.stream = p.stream;
   for (int b = 0; b < c->B; ++b) {
     a.seq[b] = ShareSeq{pos0[b], row0[b]};
     a.skip[b] = p.group_of[b] == 255 ? 0 : (uint16_t)p.tiles[p.group_of[b]];
@@ -150,9 +151,12 @@ void plan_attend(const rv_cache* c, const int* pos0, const int* row0, ShareArgs&
 
 extern "C" {
 
-rv_status rv_model_qk_norm(rv_model* m, const float* d_q_gain, const float* d_k_gain) {
+rv_status rv_model_qk_norm(rv_model* m, const float* d_q_gain, const float* d_k_gain, int64_t count) {
   if (!m) return rv_fail(RV_E_ARG, "model is NULL");
   if (!d_q_gain != !d_k_gain) return rv_fail(RV_E_ARG, "gains of queries and keys come together");
+  if (d_q_gain && count != (int64_t)m->cfg.n_layers * m->cfg.head_dim)
+    return rv_fail(RV_E_ARG, "%lld gains, the model has %d layers of head_dim %d", (long long)count, m->cfg.n_layers,
+                   m->cfg.head_dim);
   if (((uintptr_t)d_q_gain | (uintptr_t)d_k_gain) & 15) return rv_fail(RV_E_ARG, "gains must start at multiples of 16 bytes");
   m->q_gain = d_q_gain;
   m->k_gain = d_k_gain;

@@ -307,6 +307,7 @@ struct ShareArgs {
   float scale_log2;
   int nseq, rows, groups;
   SharePart sh, part;    // the shared and the own part (rv_tiles.h)
+  int stream;            // nothing shared, at most 16 queries to a kv head, more keys than the last-level cache holds
   int own_last;          // the own part fits beside the shared part's last round
   int direct;            // one run and no groups: the output is final (this and the next are the launcher's)
   int runs_sh, runs_own;  // workgroups of the two parts, in runs of 8

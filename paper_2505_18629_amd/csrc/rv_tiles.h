@@ -204,6 +204,7 @@ inline void plan_copy(int n, const uint8_t* h_src, const uint8_t* h_dst, const i
 // rows stay empty).  Every sequence then attends its remaining keys alone.
 // Both parts are split into runs of keys; the results of a row's runs (slots
 // 0 .. sh.ns-1 of the shared part, then those of its own) are merged afterwards.
+constexpr double kStreamBytes = 256e6;  // of the last-level cache
 constexpr int kShareGroups = 32;
 constexpr int kMergeSlots = 96;
 
@@ -216,6 +217,7 @@ struct SharePart {
 
 struct SharePlan {
   int nseq = 0, rows = 0, groups = 0;
+  bool stream = false;           // nothing shared, 16 queries to a kv head at most, keys beyond kStreamBytes
   bool own_last = false;         // the own part fits beside the last round of the shared part
   SharePart sh, own;
   uint8_t group_of[kMaxSlots];   // 255: none
@@ -366,6 +368,7 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
   p.sh = SharePart{std::max(p.own.qpw, qpw(most_sh)), 0, 0, 0};
   p.own.nqg = (most + p.own.qpw - 1) / p.own.qpw;
   p.sh.nqg = (most_sh + p.sh.qpw - 1) / p.sh.qpw;
+  p.stream = bf16 && !p.groups && p.own.qpw == 16 && (double)bytes * n_kv * 8 * hd > kStreamBytes;
   ShareCut a[kCuts], c[kCuts];
   const int na = p.groups ? cut_part(bf16, sh, p.groups, n_kv, hd, p.sh.qpw, std::max(1, fit / 2), a) : 1;
   if (!p.groups) a[0] = ShareCut{};

@@ -408,9 +408,12 @@ static void refusals() {
   size_t off = 9, bytes = 9;
   CHECK(rv_debug_cache_span(c, RV_SPAN_K, &off, &bytes) == RV_OK && off == 0 && bytes == h.k.size() * 4);
   CHECK(rv_debug_cache_span(c, RV_SPAN_K_LO, &off, &bytes) == RV_E_ARG && rv_debug_cache_span(c, 9, &off, &bytes) == RV_E_ARG);
-  CHECK(rv_model_qk_norm(nullptr, nullptr, nullptr) == RV_E_ARG);
-  CHECK(rv_model_qk_norm(&h.m, (const float*)mem, nullptr) == RV_E_ARG);
-  CHECK(rv_model_qk_norm(&h.m, (const float*)(mem + 4), (const float*)mem) == RV_E_ARG);
+  CHECK(rv_model_qk_norm(nullptr, nullptr, nullptr, 0) == RV_E_ARG);
+  CHECK(rv_model_qk_norm(&h.m, (const float*)mem, nullptr, 32) == RV_E_ARG);
+  CHECK(rv_model_qk_norm(&h.m, (const float*)(mem + 4), (const float*)mem, 32) == RV_E_ARG);
+  CHECK(rv_model_qk_norm(&h.m, (const float*)mem, (const float*)mem, 64) == RV_E_ARG);
+  CHECK(rv_model_qk_norm(&h.m, (const float*)mem, (const float*)mem, 32) == RV_OK && h.m.q_gain);
+  CHECK(rv_model_qk_norm(&h.m, nullptr, nullptr, 0) == RV_OK && !h.m.q_gain);
   int32_t dims[4];
   CHECK(rv_cache_dims(c, dims) == RV_OK && dims[0] == 4 && dims[1] == 4 && dims[2] == 1 && dims[3] == 32);
 }

@@ -511,3 +511,37 @@ def test_arguments_of_the_binding(rv, gpu):
         rv.rv_cache_attend(c.h, 0, [0] * 3, [1] * 3, rows_of(3, 264, 1)[:, 2:258], q[:, :256].clone())
     none = torch.empty((0, 256), device="cuda")
     rv.rv_cache_attend(c.h, 0, [0] * 3, [0] * 3, none, none)
+
+
+def test_attend_more_keys_than_the_last_level_cache(rv, gpu):
+    """Decode steps over 300 MB of keys and values (nontemporal loads), ragged; float64 on the card."""
+    import torch
+    hq, hkv, hd, B = 16, 8, 128, 33
+    lens = [1, 64, 1300] + [1000 + 7 * b for b in range(B - 3)]
+    c = Cache(rv, "bf16", hq, hkv, hd, B, 1300)
+    x = rows_of(sum(lens), 2 * hkv * hd, 41)
+    rv.rv_cache_append(c.h, 0, [0] * B, lens, None, x[:, :hkv * hd], x[:, hkv * hd:], None, rotate=False)
+    k, v = (torch.empty((sum(lens), hkv * hd), device="cuda") for _ in range(2))
+    rv.rv_cache_read(c.h, 0, [0] * B, lens, k, v)
+    q = rows_of(B, hq * hd, 42)
+    out = torch.empty_like(q)
+    rv.rv_cache_attend(c.h, 0, [n - 1 for n in lens], [1] * B, q, out)
+    ref, at = torch.empty((B, hq, hd), dtype=torch.float64, device="cuda"), 0
+    for b, n in enumerate(lens):
+        kk, vv = (t[at:at + n].double().view(n, hkv, hd).transpose(0, 1) for t in (k, v))
+        s = (kk @ q[b].double().view(hkv, hq // hkv, hd).transpose(1, 2).contiguous()) / hd ** 0.5
+        ref[b] = (torch.softmax(s, 1).transpose(1, 2) @ vv).reshape(hq, hd)
+        at += n
+    assert float(torch.linalg.norm(out.view(B, hq, hd).double() - ref)) < 2e-5 * float(torch.linalg.norm(ref))
+
+
+@pytest.mark.parametrize("counts", [[700, 0, 1, 1, 0, 3], [1] * 6, [0, 0, 0, 0, 0, 9]])
+def test_attend_rows_of_few_sequences(rv, gpu, counts):
+    """One sequence with many rows among others with few or none, over a prompt that all share."""
+    import torch
+    case = ("bf16", "f32", (4, 2, 64), [70 + 3 * b for b in range(6)], counts, [(0, 65, [1, 2, 3, 4, 5])])
+    c = filled(rv, case)
+    q = rows_of(sum(counts), 4 * 64, 43)
+    out = torch.empty_like(q)
+    rv.rv_cache_attend(c.h, 0, case[3], counts, q, out)
+    check_attend(rv, c, case, out, q)
