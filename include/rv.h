@@ -258,7 +258,7 @@ typedef struct {
   int32_t rotate;                     /* 0: keys (and queries) are stored as they are */
   int64_t n_rows, q_width, kv_width;  /* q_width: n_heads * head_dim, or 0 without queries */
   const void *d_q, *d_k, *d_v;        /* d_q may be NULL */
-  void* d_q_out;                      /* queries, normalised and rotated; may be d_q; NULL with d_q */
+  void* d_q_out;                      /* queries, normalised and rotated; d_q with ld_q_out == ld_q, or apart from it; NULL with d_q */
   int64_t ld_q, ld_k, ld_v, ld_q_out;
   const float *d_q_gain, *d_k_gain;   /* [head_dim] fp32 at multiples of 16 bytes, or NULL: that side is not normalised */
 } rv_rows;
@@ -307,7 +307,7 @@ rv_status rv_cache_fork(rv_cache* c, int32_t src, int32_t len, int32_t n, const 
  * by 1 / sqrt(head_dim) here), query head h with kv head h / (n_heads /
  * n_kv_heads).  Tiles that several sequences of the call share are read once for
  * all their rows.  At most as many rows as the workspace holds: max(batch *
- * max_block, 2048) (else RV_E_CAPACITY).  d_out may be d_q.  Asynchronous. */
+ * max_block, 2048) (else RV_E_CAPACITY).  d_out may be d_q, with ld_out == ld_q.  Asynchronous. */
 rv_status rv_cache_attend(const rv_cache* c, int32_t layer, int32_t batch, const int32_t* h_pos, const int32_t* h_rows,
                           int32_t dtype, int64_t n_rows, int64_t width, const void* d_q, int64_t ld_q, void* d_out,
                           int64_t ld_out, void* stream);

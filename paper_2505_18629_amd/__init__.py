@@ -289,18 +289,22 @@ def _spans(positions, counts):
     return batch, pos, n
 
 
-def _row_tensors(here: int, a, *others) -> int:
-    """Type of the rows of tensors of one type on the current device, each dense within a row."""
-    dtype, rows = a.dtype, a.shape[0]
+def _row_tensors(here: int, *tensors):
+    """(type, rows, and each one's width, address and row stride) of row tensors of one
+    type on the current device, each dense within a row."""
+    dtype, rows = tensors[0].dtype, tensors[0].shape[0] if tensors[0].dim() == 2 else -1
     kind = _ROW_TYPES.get(dtype)
     if kind is None:
         raise ValueError(f"rows must be float32 or bfloat16, not {dtype}")
-    for t in (a,) + others:
-        if t.dtype != dtype or t.get_device() != here or t.dim() != 2 or t.shape[0] != rows or \
-                (t.stride(1) != 1 and rows):
+    out = [kind, rows]
+    for t in tensors:
+        shape, strides = t.shape, t.stride()
+        if t.dtype != dtype or t.get_device() != here or len(shape) != 2 or shape[0] != rows or \
+                (strides[1] != 1 and rows):
             raise ValueError(f"expected {rows} rows of {dtype} on cuda:{here} (the current device), dense within a row, "
-                             f"got {tuple(t.shape)} of {t.dtype} with strides {t.stride()} on {t.device}")
-    return kind
+                             f"got {tuple(shape)} of {t.dtype} with strides {strides} on {t.device}")
+        out += (shape[1], t.data_ptr(), strides[0])
+    return out
 
 
 def _gain(t, hd: int) -> Optional[int]:
@@ -325,28 +329,28 @@ def rv_cache_append(cache: int, layer: int, positions, counts, q, k, v, q_out, q
     """q and q_out may be None together; q_out may be q."""
     here = torch.cuda.current_device()
     batch, pos, n = _spans(positions, counts)
-    rows, width = k.shape
-    if v.shape != k.shape or (q is None) != (q_out is None) or (q is not None and q.shape != q_out.shape):
+    if (q is None) != (q_out is None):
+        raise ValueError("q and its output come together")
+    if q is None:
+        kind, rows, wk, pk, ldk, wv, pv, ldv = _row_tensors(here, k, v)
+        wq = wo = ldq = ldo = 0
+        pq = po = None
+    else:
+        kind, rows, wk, pk, ldk, wv, pv, ldv, wq, pq, ldq, wo, po, ldo = _row_tensors(here, k, v, q, q_out)
+    if wk != wv or wq != wo:
         raise ValueError("k and v, and q and its output, have the same shape")
     hd = 0 if q_gain is None and k_gain is None else rv_cache_dims(cache)[3]
-    if q is None:
-        a = rv_rows(_row_tensors(here, k, v), rotate, rows, 0, width, None, k.data_ptr(), v.data_ptr(), None, 0, k.stride(0),
-                    v.stride(0), 0, _gain(q_gain, hd), _gain(k_gain, hd))
-    else:
-        a = rv_rows(_row_tensors(here, k, v, q, q_out), rotate, rows, q.shape[1], width, q.data_ptr(), k.data_ptr(),
-                    v.data_ptr(), q_out.data_ptr(), q.stride(0), k.stride(0), v.stride(0), q_out.stride(0),
-                    _gain(q_gain, hd), _gain(k_gain, hd))
+    a = rv_rows(kind, rotate, rows, wq, wk, pq, pk, pv, po, ldq, ldk, ldv, ldo, _gain(q_gain, hd), _gain(k_gain, hd))
     _check(_lib.rv_cache_append(cache, layer, batch, pos, n, ctypes.byref(a), _stream_on(here, stream)))
 
 
 def rv_cache_read(cache: int, layer: int, positions, counts, k, v, stream=None) -> None:
     here = torch.cuda.current_device()
     batch, pos, n = _spans(positions, counts)
-    if v.shape != k.shape:
+    kind, rows, wk, pk, ldk, wv, pv, ldv = _row_tensors(here, k, v)
+    if wk != wv:
         raise ValueError("k and v have the same shape")
-    kind = _row_tensors(here, k, v)
-    _check(_lib.rv_cache_read(cache, layer, batch, pos, n, kind, k.shape[0], k.shape[1], k.data_ptr(), k.stride(0),
-                              v.data_ptr(), v.stride(0), _stream_on(here, stream)))
+    _check(_lib.rv_cache_read(cache, layer, batch, pos, n, kind, rows, wk, pk, ldk, pv, ldv, _stream_on(here, stream)))
 
 
 def rv_cache_copy(cache: int, src, dst, lengths, stream=None) -> None:
@@ -365,11 +369,11 @@ def rv_cache_attend(cache: int, layer: int, positions, counts, q, out, stream=No
     """out may be q."""
     here = torch.cuda.current_device()
     batch, pos, n = _spans(positions, counts)
-    if out.shape != q.shape:
+    kind, rows, wq, pq, ldq, wo, po, ldo = _row_tensors(here, q, out)
+    if wq != wo:
         raise ValueError("q and the output have the same shape")
-    kind = _row_tensors(here, q, out)
-    _check(_lib.rv_cache_attend(cache, layer, batch, pos, n, kind, q.shape[0], q.shape[1], q.data_ptr(), q.stride(0),
-                                out.data_ptr(), out.stride(0), _stream_on(here, stream)))
+    _check(_lib.rv_cache_attend(cache, layer, batch, pos, n, kind, rows, wq, pq, ldq, po, ldo,
+                                _stream_on(here, stream)))
 
 
 def rv_model_qk_norm(model: int, q_gain, k_gain) -> None:

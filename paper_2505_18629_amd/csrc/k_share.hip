@@ -46,6 +46,7 @@ RV_DEV bool unit_of(const ShareArgs& a, int x, Unit& u) {
   u.q_begin = qg * sp.qpw;
   if (PART) {
     if (i >= a.nseq) return false;
+    if (a.sorted) i = a.order[i];
     u.pos0 = a.seq[i].pos0;
     u.row0 = a.seq[i].row0;
     u.nq = (a.seq[i + 1].row0 - u.row0) * G;

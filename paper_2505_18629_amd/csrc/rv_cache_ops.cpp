@@ -136,6 +136,8 @@ void plan_attend(const rv_cache* c, const int* pos0, const int* row0, ShareArgs&
   a.part = p.own;
   a.own_last = p.own_last;
   a.stream = p.stream;
+  a.sorted = p.sorted;
+  if (p.sorted) std::copy(p.order, p.order + c->B, a.order);
   for (int b = 0; b < c->B; ++b) {
     a.seq[b] = ShareSeq{pos0[b], row0[b]};
     a.skip[b] = p.group_of[b] == 255 ? 0 : (uint16_t)p.tiles[p.group_of[b]];
@@ -193,6 +195,7 @@ rv_status rv_cache_append(rv_cache* c, int32_t layer, int32_t batch, const int32
   if (rows->d_q) {
     if (rv_status s = check_rows("q", rows->d_q, rows->ld_q, rows->q_width, qd, io); s != RV_OK) return s;
     if (rv_status s = check_rows("q output", rows->d_q_out, rows->ld_q_out, rows->q_width, qd, io); s != RV_OK) return s;
+    if (rows->d_q_out == rows->d_q && rows->ld_q_out != rows->ld_q) return rv_fail(RV_E_ARG, "q in place with two row strides");
   }
   if (((uintptr_t)rows->d_q_gain | (uintptr_t)rows->d_k_gain) & 15)
     return rv_fail(RV_E_ARG, "gains must start at multiples of 16 bytes");
@@ -381,6 +384,7 @@ rv_status rv_cache_attend(const rv_cache* c, int32_t layer, int32_t batch, const
   const int qd = mc.n_heads * mc.head_dim;
   if (rv_status s = check_rows("q", d_q, ld_q, width, qd, dtype); s != RV_OK) return s;
   if (rv_status s = check_rows("output", d_out, ld_out, width, qd, dtype); s != RV_OK) return s;
+  if (d_out == d_q && ld_out != ld_q) return rv_fail(RV_E_ARG, "q in place with two row strides");
   ShareArgs a{};
   plan_attend(c, pos, row0, a);
   const Planes p = layer_planes(c, layer);

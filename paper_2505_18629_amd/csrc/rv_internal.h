@@ -307,9 +307,10 @@ struct ShareArgs {
   float scale_log2;
   int nseq, rows, groups;
   SharePart sh, part;    // the shared and the own part (rv_tiles.h)
-  int stream;            // nothing shared, at most 16 queries to a kv head, more keys than the last-level cache holds
-  int own_last;          // the own part fits beside the shared part's last round
-  int direct;            // one run and no groups: the output is final (this and the next are the launcher's)
+  bool stream;           // nothing shared, at most 16 queries to a kv head, more keys than the last-level cache holds
+  bool own_last;         // the own part fits beside the shared part's last round
+  bool sorted;           // the own part's workgroups go by `order`
+  bool direct;           // one run and no groups: the output is final (this and the next are the launcher's)
   int runs_sh, runs_own;  // workgroups of the two parts, in runs of 8
   int lead_sh, lead_own;  // how many of each start first
   // What follows lies in other cache lines of the kernel arguments, which live in
@@ -319,6 +320,7 @@ struct ShareArgs {
   ShareSeq seq[RV_MAX_BATCH + 1];
   uint16_t skip[RV_MAX_BATCH];  // tiles that the sequence's group attends for it
   uint8_t member[RV_MAX_BATCH];
+  uint8_t order[RV_MAX_BATCH];  // sequences by their own keys, most first
   int16_t first[kShareGroups + 1];
   int32_t tiles[kShareGroups], rmax[kShareGroups];
 };

@@ -220,6 +220,11 @@ struct SharePlan {
   bool stream = false;           // nothing shared, 16 queries to a kv head at most, keys beyond kStreamBytes
   bool own_last = false;         // the own part fits beside the last round of the shared part
   SharePart sh, own;
+  // more workgroups of the own part than run at once: they start in `order`, long ones
+  // first (64 sequences of 16-2000 keys, one row each, 8B: 104.2 -> 94.1 us; without
+  // need the lookup costs 0.5 us of 37)
+  bool sorted = false;
+  uint8_t order[kMaxSlots];      // sequences by their own keys, most first
   uint8_t group_of[kMaxSlots];   // 255: none
   uint8_t member[kMaxSlots];     // members, group after group
   int16_t first[kShareGroups + 1];
@@ -299,6 +304,12 @@ constexpr int kCuts = sizeof kCutCounts / sizeof kCutCounts[0];
 // shared part leave the other CUs enough time, 253 us; 192 do not, 296).
 constexpr double kBeside = 1.35;
 
+// Two workgroups share a CU where registers and LDS hold them (head_dim 64 and less,
+// 128 queries a workgroup), and do this much more than one.  (16 sequences of
+// 300-1900 keys, 1-9 rows each at the 1B shape: 2 runs, one workgroup per CU, 26.8 us;
+// 3: 24.0, 4: 22.4, 6: 25.7, 8: 26.4.)
+constexpr double kPair = 1.25;
+
 // us of a workgroup that attends `keys` keys: prologue, epilogue and latencies,
 // then the keys at its rate (head_dim 128; others in proportion).
 inline double share_wg_us(bool bf16, int qpw, int keys, int hd) {
@@ -347,15 +358,16 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
   plan_groups(tl, pos0, row0, p);
   const int fit = (int)std::min<size_t>(kMergeSlots, part_entries / ((size_t)p.rows * n_heads));
   ShareUnit own[kMaxSlots], sh[kShareGroups];
-  int n = 0, most = 0, most_sh = 0;
+  int n = 0, most = 0, most_sh = 0, keys[kMaxSlots] = {};  // of each sequence's own part
   long long bytes = 0;
   for (int b = 0; b < B; ++b) {
     const int r = row0[b + 1] - row0[b];
     if (!r) continue;
     const int t0 = p.group_of[b] == 255 ? 0 : p.tiles[p.group_of[b]];
-    own[n++] = ShareUnit{pos0[b] + r - t0 * kTile, r * G};
+    keys[b] = pos0[b] + r - t0 * kTile;
+    own[n++] = ShareUnit{keys[b], r * G};
     most = std::max(most, r * G);
-    bytes += own[n - 1].keys;
+    bytes += keys[b];
   }
   for (int g = 0; g < p.groups; ++g) {
     sh[g] = ShareUnit{p.tiles[g] * kTile, (p.first[g + 1] - p.first[g]) * p.rmax[g] * G};
@@ -373,7 +385,8 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
   const int na = p.groups ? cut_part(bf16, sh, p.groups, n_kv, hd, p.sh.qpw, std::max(1, fit / 2), a) : 1;
   if (!p.groups) a[0] = ShareCut{};
   const int nc = cut_part(bf16, own, n, n_kv, hd, p.own.qpw, std::max(1, fit - (p.groups ? 1 : 0)), c);
-  const double stream = (double)bytes * n_kv * 8 * hd / 5.2e6, slots = bf16 ? 256 : 2048;
+  const bool pair = bf16 && hd <= 64 && p.own.qpw == 128 && p.sh.qpw == 128;
+  const double stream = (double)bytes * n_kv * 8 * hd / 5.2e6, slots = bf16 ? pair ? 512 : 256 : 2048;
   double best = 0;
   for (int i = 0; i < na; ++i)
     for (int j = 0; j < nc; ++j) {
@@ -385,6 +398,7 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
       if (!rounds) t = c[j].wgs <= slots ? c[j].longest : c[j].sum / slots + c[j].longest / 2;
       else if (beside > gap) t += (beside - gap) / slots + c[j].longest / 2;
       t = std::max(std::max(t, c[j].longest), stream);
+      if (pair) t = std::max(t, (a[i].sum + c[j].sum) / (256 * kPair));
       if (runs > 1) t += 5.0 + 0.1 * runs + (double)runs * p.rows * n_heads * hd * 8 / 3.5e6;
       if ((!i && !j) || t < best) {
         best = t;
@@ -393,6 +407,10 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
         p.own.ks = c[j].ks;
         p.own.ns = c[j].ns;
         p.own_last = beside <= gap;
+        p.sorted = c[j].wgs > slots;
       }
     }
+  if (!p.sorted) return;
+  for (int b = 0; b < B; ++b) p.order[b] = (uint8_t)b;
+  std::sort(p.order, p.order + B, [&](int x, int y) { return keys[x] != keys[y] ? keys[x] > keys[y] : x < y; });
 }

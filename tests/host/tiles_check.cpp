@@ -322,6 +322,40 @@ static void shares() {
   CHECK(grouped > 200);
 }
 
+// Many sequences: the order of the own part's workgroups names each once, most keys first.
+static void orders() {
+  std::mt19937 r(5);
+  int sorted = 0;
+  for (int it = 0; it < 60; ++it) {
+    const int B = 2 + r() % 255, n_kv = 8;
+    TileOwners tl;
+    tl.create(B, 40);
+    if (it % 2)
+      for (int b = 1; b < B; ++b)
+        for (int t = 0; t < 20; ++t) tl.set(b, t, 0);
+    int pos[256], row0[257] = {0};
+    for (int b = 0; b < B; ++b) {
+      const int n = r() % 8 ? 1 : 0;
+      pos[b] = n ? 20 * 64 + r() % (20 * 64) : 0;
+      row0[b + 1] = row0[b] + n;
+    }
+    if (!row0[B]) continue;
+    SharePlan p;
+    plan_share(tl, it % 3, pos, row0, 32, n_kv, 128, (size_t)2048 * 32 * 8, p);
+    if (!p.sorted) continue;
+    ++sorted;
+    std::vector<int> met(B);
+    int before = 0x7fffffff;
+    for (int i = 0; i < B; ++i) {
+      const int b = p.order[i], n = row0[b + 1] - row0[b];
+      const int keys = n ? pos[b] + n - (p.group_of[b] == 255 ? 0 : p.tiles[p.group_of[b]] * 64) : 0;
+      CHECK(!met[b]++ && keys <= before);
+      before = keys;
+    }
+  }
+  CHECK(sorted > 20);
+}
+
 alignas(16) static char mem[64];
 static void refusals() {
   Host h(4, 200);
@@ -344,6 +378,7 @@ static void refusals() {
   CHECK((r = ok, r.dtype = RV_BF16, r.ld_q = 132, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.d_q_out = nullptr, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.ld_q_out = 127, append(r)) == RV_E_ARG);
+  CHECK((r = ok, r.ld_q_out = 132, append(r)) == RV_E_ARG);  // in place with another stride
   CHECK((r = ok, r.n_rows = 2, append(r)) == RV_E_ARG && (r = ok, r.q_width = 96, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.kv_width = 28, append(r)) == RV_E_ARG);
   CHECK((r = ok, r.d_k_gain = (const float*)(mem + 4), append(r)) == RV_E_ARG);
@@ -372,6 +407,7 @@ static void refusals() {
   CHECK(attend(3, 7) == RV_E_ARG && attend(3, RV_F32, nullptr) == RV_E_ARG && attend(2) == RV_E_ARG);
   CHECK(attend(3, RV_F32, mem, 64) == RV_E_ARG && attend(3, RV_F32, mem, 128, 64) == RV_E_ARG);
   CHECK(attend(3, RV_F32, mem, 128, 128, 1) == RV_E_ARG);
+  CHECK(attend(3, RV_F32, mem, 128, 132) == RV_E_ARG);  // in place with another stride
   CHECK(g_launches == 0);
   const int32_t none[4] = {0, 0, 0, 0};
   CHECK(rv_cache_attend(c, 0, 4, pos, none, RV_F32, 0, 128, nullptr, 0, nullptr, 0, nullptr) == RV_OK && g_launches == 0);
@@ -419,6 +455,7 @@ static void refusals() {
 }
 
 int main() {
+  orders();
   refusals();
   programs();
   for (unsigned s = 0; s < 12; ++s) walk(2 + s % 6, s % 3 ? 64 * (1 + s % 4) + s : 64 * (1 + s % 3), 250, s);

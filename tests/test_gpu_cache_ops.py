@@ -545,3 +545,29 @@ def test_attend_rows_of_few_sequences(rv, gpu, counts):
     out = torch.empty_like(q)
     rv.rv_cache_attend(c.h, 0, case[3], counts, q, out)
     check_attend(rv, c, case, out, q)
+
+
+@pytest.mark.parametrize("dtype,hkv,B", [("bf16", 4, 80), ("f32", 16, 150)])
+def test_attend_many_forks_of_unlike_lengths(rv, gpu, dtype, hkv, B):
+    """More sequences than run at once: their workgroups start in the order of their keys."""
+    import torch
+    counts = [0 if b % 11 == 3 else 1 + b % 2 for b in range(B)]
+    case = (dtype, "f32", (hkv, hkv, 32), [66 + b * 37 % 300 for b in range(B)], counts, [(0, 66, list(range(2, B, 2)))])
+    c = filled(rv, case)
+    q = rows_of(sum(counts), hkv * 32, 44)
+    out = torch.empty_like(q)
+    rv.rv_cache_attend(c.h, 0, case[3], counts, q, out)
+    check_attend(rv, c, case, out, q)
+
+
+def test_attend_in_place_with_two_strides(rv, gpu):
+    import torch
+    c = filled(rv, ("bf16", "f32", (4, 2, 64), [70, 3], [1, 2], []))
+    wide = rows_of(3, 512, 45)
+    flat = wide.view(-1)[:3 * 256].view(3, 256)
+    with pytest.raises(rv.RVError, match="RV_E_ARG"):
+        rv.rv_cache_attend(c.h, 0, [70, 3], [1, 2], wide[:, :256], flat)
+    apart = torch.empty((3, 256), device="cuda")
+    rv.rv_cache_attend(c.h, 0, [70, 3], [1, 2], wide[:, :256], apart)
+    rv.rv_cache_attend(c.h, 0, [70, 3], [1, 2], wide[:, :256], wide[:, :256])
+    assert torch.equal(wide[:, :256], apart)
