@@ -21,18 +21,24 @@ RV_DEV int find_seq(const int* blk0, int B, int x) {
   return n - 1;
 }
 
-// 8 consecutive values of a row of fp32 or bf16 as fp32, and back.
-template <int IO>
+template <bool ONCE, typename V>
+RV_DEV V load_vec(const V* p) {
+  return ONCE ? __builtin_nontemporal_load(p) : *p;
+}
+// 8 consecutive values of a row of fp32 or bf16 as fp32, and back.  ONCE: a row
+// that nothing reads after this kernel, past the L2 (see k_append).
+template <int IO, bool ONCE = false>
 RV_DEV void load8(const void* p, size_t i, float (&x)[8]) {
   if constexpr (IO == RV_F32) {
-    const f32x4_t a = *(const f32x4_t*)((const float*)p + i), b = *(const f32x4_t*)((const float*)p + i + 4);
+    const f32x4_t a = load_vec<ONCE>((const f32x4_t*)((const float*)p + i));
+    const f32x4_t b = load_vec<ONCE>((const f32x4_t*)((const float*)p + i + 4));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       x[j] = a[j];
       x[4 + j] = b[j];
     }
   } else {
-    const u32x4 r = *(const u32x4*)((const uint16_t*)p + i);
+    const u32x4 r = load_vec<ONCE>((const u32x4*)((const uint16_t*)p + i));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       x[2 * j] = __uint_as_float(r[j] << 16);
@@ -94,6 +100,12 @@ RV_DEV bool group_touched(int g, int k_lo, int k_hi) {
 // rows go through LDS and each thread writes the 8 positions of a (dim, slot
 // group) with one store -- 2-byte stores of single positions remain for the
 // groups that the rows fill in part.
+//
+// Bound by HBM for prompts: 6 of 300-1100 tokens at the 8B shape in bf16, 148 MB,
+// 31 us (4.7 TB/s; 36 with plain loads of the rows, 37 with nontemporal stores of K
+// and V, which are read soon; heads four a batch take 2.5 more than two, one a batch
+// 0.4).  A verify block (4 x 43 fp32 rows, 14B) takes 6.5 us, a few rows 3.5: launch,
+// arguments, row, store.
 constexpr int kHeadBatch = 2, kHeadRounds = 4;
 template <int DT, int IO, int HD>
 __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
@@ -134,8 +146,8 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
         const bool is_q = h < a.n_heads;
         const void* src = is_q ? a.q : a.k;
         const size_t at = (size_t)(row_lo + r) * (is_q ? a.ldq : a.ldk) + (size_t)(is_q ? h : h - a.n_heads) * HD + d;
-        load8<IO>(src, at, y1[u]);
-        load8<IO>(src, at + HALF, y2[u]);
+        load8<IO, true>(src, at, y1[u]);
+        load8<IO, true>(src, at + HALF, y2[u]);
       }
 #pragma unroll
       for (int u = 0; u < kHeadBatch; ++u) {
@@ -189,7 +201,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   for (int i = tid; i < rows * (HD / 8); i += 256) {
     const int r = i / (HD / 8), d = i % (HD / 8) * 8;
     float y[8];
-    load8<IO>(a.v, (size_t)(row_lo + r) * a.ldv + (size_t)hh * HD + d, y);
+    load8<IO, true>(a.v, (size_t)(row_lo + r) * a.ldv + (size_t)hh * HD + d, y);
     if constexpr (DT == RV_F32) {
       store8<RV_F32>(a.vc, base + (size_t)(p_lo + r) * HD + d, y);
     } else {
@@ -231,7 +243,8 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
 
 // ----------------------------------------------------------- read
 // The inverse for K and V: cached rows as values (hi + lo), wherever the tile
-// lies.  Workgroups as above over the k and v heads.
+// lies.  Workgroups as above over the k and v heads.  Bound by HBM or the
+// last-level cache (the prompts above, just appended, as bf16: 11.5 us).
 template <int DT, int IO, int HD>
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   __shared__ float sv[kBlockPos][HD + 1];
@@ -324,7 +337,10 @@ RV_DEV void run_moves(const CopyProgram& p, int unit, Addr addr, On on, int step
 // one head is one contiguous span of a slot in every cache layout.  Lengths
 // count committed tokens: K and V of positions 0 .. len-2 come in whole tiles,
 // the ids 0 .. len-1 one by one (further workgroups, a thread each), and the
-// sequence's bad-id flag with them (one more).
+// sequence's bad-id flag with them (one more).  Bound by HBM: 16 sequences of
+// 512-2048 tokens in a new order, 8 layers of the 8B shape, 2.38 GB read and
+// written in 519 us (4.6 TB/s; a large copy reaches 5.5; 546 with kCopyVecs 2, 531 with 8,
+// 535 with plain stores).
 constexpr int kCopyVecs = 4;  // 16-byte values per thread and move
 __global__ __launch_bounds__(256) void k_copy(CopyArgs a) {
   const int unit = blockIdx.y, tid = threadIdx.x;
