@@ -267,13 +267,20 @@ RV_DEV void take_out(u32x4 (&vh)[ND], u32x4 (&vl)[ND], int k0, int kend, const Q
 
 // ----------------------------------------------------------- bf16, many queries
 // S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMAs, operands as pairs of planes
-// (three products each, lo lo dropped: 2^-16 of the result; queries given in
-// bf16 have no lo plane, two products).  8 waves of TPW 16-query tiles: every
+// hi = bf16(x), lo = bf16(x - hi), as the cache holds K and V: a pair is within
+// 2^-17 of x, and with lo lo dropped (2^-16 of a product) fp32 rows come out within
+// 5e-6 of the exact result (fp32 MFMAs would cost 2.6 times these products:
+// 153 against 1198 / 3 TFLOP/s in library products).  Three products each; queries given in bf16 have no lo
+// plane, two products.  Scores, statistics and sums are fp32.  8 waves of TPW 16-query tiles: every
 // K and V operand read from LDS serves TPW tiles, and with one LDS reads bound
 // the kernel (512 KiB a tile and CU against 3072 cycles of MFMA), so calls with
 // more than 128 queries take two.  The cache holds tiles in operand order (k_elem
 // / v_elem): a 64-key tile is four spans that go global -> LDS directly,
 // double-buffered.
+// Bound by the matrix cores' power: 64 continuations of 32768 shared keys (70B
+// shape, fp32 rows) take 252 us with their own keys and the merge, 1.12 PFLOP/s of
+// products in the shared part, where a large library product reaches 1.20.  16
+// blocks of 31 rows over 2048 shared keys (8B) 67 us.
 template <int HD, int PART, int TPW, bool QLO>
 RV_DEV void attend_many(const ShareArgs& a, const Unit& u, uint16_t (&sm0)[4][kKB * HD], uint16_t (&sm1)[4][kKB * HD]) {
   constexpr int NW = 8, DC = HD / 32, DT = HD / 16, SPAN = kKB * HD;
@@ -447,7 +454,9 @@ RV_DEV void attend_many(const ShareArgs& a, const Unit& u, uint16_t (&sm0)[4][kK
 // ----------------------------------------------------------- bf16, at most 16 queries
 // Decode steps: the 8 waves share the 16 queries and split the keys, wave w
 // taking tiles w, w + 8, ... of KT keys straight to registers; their states
-// merge in LDS.  STREAM: nontemporal loads, for calls whose keys exceed the
+// merge in LDS.  Bound by what a CU draws from HBM: 640 keys of one kv head in 19 us
+// (34 GB/s a CU), 64 sequences of 16-2000 keys 94 us with the merge (5.9 TB/s); one
+// sequence of 1024 keys 8 us, latency.  STREAM: nontemporal loads, for calls whose keys exceed the
 // last-level cache anyway (64 sequences of 1000 keys, 524 MB: 110 -> 98 us at the
 // 70B shape, 101 -> 91 at 8B; with 112 MB, 33.2 -> 34.8).
 // red: 8 x 16 x HD values in LDS, 16-byte columns xor-ed with the query so that
@@ -649,7 +658,8 @@ RV_DEV void take_out_f32(float (&v)[DC], bool vis, f32x4_t (&o)[DC]) {
 // straight from the row-major cache.  The k slots of an MFMA may hold any four
 // dims that both operands agree on, so a lane's 16-byte load of dims
 // 16c + 4(l/16) .. +3 feeds four MFMAs, and P comes straight from the scores.
-// Bound by latency: all loads of KT keys, K and V, are issued together.
+// Bound by latency: all loads of KT keys, K and V, are issued together (four blocks
+// of 21 rows over 128 shared keys, 8 heads of 64: 8.5 us).
 template <int HD, int PART>
 RV_DEV void attend_f32(const ShareArgs& a, const Unit& u) {
   constexpr int DC = HD / 16, KT = HD == 128 ? 32 : 64, NB = KT / 16;
@@ -776,7 +786,8 @@ __global__ __launch_bounds__(64) void k_share_f32(ShareArgs a) {
 // ----------------------------------------------------------- merge
 // hd / 4 lanes per (row, head), a workgroup per row and 1024 / hd heads: one pass
 // over the runs that had keys for the row, shared runs first, in batches whose
-// loads are issued together.
+// loads are issued together.  Latency bound for few rows (4 us), else by its bytes
+// (16 x 31 rows x 4 runs, 8B: 33 MB, 9 us).
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void k_share_merge(ShareArgs a, int head_groups) {
   constexpr int LPQ = HD / 4, BATCH = 8;

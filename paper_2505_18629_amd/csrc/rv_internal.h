@@ -315,8 +315,8 @@ struct ShareArgs {
   int lead_sh, lead_own;  // how many of each start first
   // What follows lies in other cache lines of the kernel arguments, which live in
   // host memory: a workgroup reads one pair of records, and the rest only where
-  // tiles are shared (one decode step of one sequence, 128 workgroups, 8.3 us
-  // with separate arrays).
+  // tiles are shared (one decode step of one sequence, 128 workgroups: 8.0 us, 8.3
+  // with an array for each field).
   ShareSeq seq[RV_MAX_BATCH + 1];
   uint16_t skip[RV_MAX_BATCH];  // tiles that the sequence's group attends for it
   uint8_t member[RV_MAX_BATCH];

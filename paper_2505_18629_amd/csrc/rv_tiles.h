@@ -314,7 +314,9 @@ constexpr double kPair = 1.25;
 // then the keys at its rate (head_dim 128; others in proportion).
 inline double share_wg_us(bool bf16, int qpw, int keys, int hd) {
   const double f = hd / 128.0;
-  if (!bf16) return 2.5 + (keys + kTile - 1) / kTile * 1.5 * f;      // a wave of 16 queries
+  // a wave of 16 queries, latency and products in turn (1024 keys, one row: head_dim 64
+  // 52 us in one run, 13.5 in 8; 128: 92 and 19)
+  if (!bf16) return 3.5 + (keys + kTile - 1) / kTile * (0.6 + 5.2 * f);
   if (qpw == 16) return 4.0 + keys * 8.0 * hd / 4.0e4;               // what one CU draws
   return 5.0 + (keys + kTile - 1) / kTile * (qpw == 128 ? 2.6 : 5.3) * f;
 }
@@ -386,7 +388,7 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
   if (!p.groups) a[0] = ShareCut{};
   const int nc = cut_part(bf16, own, n, n_kv, hd, p.own.qpw, std::max(1, fit - (p.groups ? 1 : 0)), c);
   const bool pair = bf16 && hd <= 64 && p.own.qpw == 128 && p.sh.qpw == 128;
-  const double stream = (double)bytes * n_kv * 8 * hd / 5.2e6, slots = bf16 ? pair ? 512 : 256 : 2048;
+  const double stream = (double)bytes * n_kv * 8 * hd / 5.2e6, slots = bf16 ? pair ? 512 : 256 : 1024;
   double best = 0;
   for (int i = 0; i < na; ++i)
     for (int j = 0; j < nc; ++j) {
