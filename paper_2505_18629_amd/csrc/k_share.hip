@@ -36,8 +36,8 @@ RV_DEV bool unit_of(const ShareArgs& a, int x, Unit& u) {
   const SharePart& sp = PART ? a.part : a.sh;
   // query groups of one (run, sequence, kv head) are 8 workgroups apart: the
   // same XCD, whose L2 then holds their tiles
-  const int j = x / 8, per = j / sp.nqg, qg = j % sp.nqg;
-  int i = per * 8 + x % 8;
+  const int j = sp.spread ? x : x / 8, per = j / sp.nqg, qg = j % sp.nqg;
+  int i = sp.spread ? per : per * 8 + x % 8;
   const int run = i % sp.ns;
   i /= sp.ns;
   u.kvh = i % a.n_kv;
@@ -844,7 +844,10 @@ void launch_kinds(const ShareArgs& a, hipStream_t st) {
 int kind_of(const SharePart& p) { return p.qpw == 16 ? KIND_FEW : p.qpw == 128 ? KIND_MANY : KIND_MANY2; }
 
 // Workgroups of a part, in runs of 8.
-size_t part_runs(const SharePart& p, int n, int n_kv) { return ((size_t)p.ns * n_kv * n + 7) / 8 * p.nqg; }
+size_t part_runs(const SharePart& p, int n, int n_kv) {
+  const size_t units = (size_t)p.ns * n_kv * n;
+  return p.spread ? (units * p.nqg + 7) / 8 : (units + 7) / 8 * p.nqg;
+}
 
 template <int HD>
 hipError_t launch_all(int dtype, ShareArgs& a, hipStream_t st) {

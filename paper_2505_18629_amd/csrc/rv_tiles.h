@@ -213,6 +213,11 @@ struct SharePart {
   int nqg = 0;   // query groups of the largest unit
   int ks = 0;    // keys per run (multiple of 64)
   int ns = 0;    // runs of the longest unit
+  // query groups of one (run, sequence, kv head) lie on one XCD (8 workgroups apart),
+  // unless that would leave a quarter of the XCDs' turns empty: one group over 2 kv
+  // heads, 165 query groups, on 2 of the 8 XCDs take 31 us, spread 19 (fp32)
+  bool spread = false;
+  void place(int units) { spread = (units + 7) / 8 * 8 - units > (units + 7) / 8 * 2; }
 };
 
 struct SharePlan {
@@ -378,8 +383,9 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
   }
   // queries per workgroup: never fewer of the shared part than of the own part
   auto qpw = [&](int q) { return !bf16 || q <= 16 ? 16 : q <= 128 ? 128 : 256; };
-  p.own = SharePart{qpw(most), 0, 0, 0};
-  p.sh = SharePart{std::max(p.own.qpw, qpw(most_sh)), 0, 0, 0};
+  p.own = p.sh = SharePart{};
+  p.own.qpw = qpw(most);
+  p.sh.qpw = std::max(p.own.qpw, qpw(most_sh));
   p.own.nqg = (most + p.own.qpw - 1) / p.own.qpw;
   p.sh.nqg = (most_sh + p.sh.qpw - 1) / p.sh.qpw;
   p.stream = bf16 && !p.groups && p.own.qpw == 16 && (double)bytes * n_kv * 8 * hd > kStreamBytes;
@@ -412,6 +418,8 @@ inline void plan_share(const TileOwners& tl, bool bf16, const int32_t* pos0, con
         p.sorted = c[j].wgs > slots;
       }
     }
+  p.sh.place(p.sh.ns * n_kv * p.groups);
+  p.own.place(p.own.ns * n_kv * B);
   if (!p.sorted) return;
   for (int b = 0; b < B; ++b) p.order[b] = (uint8_t)b;
   std::sort(p.order, p.order + B, [&](int x, int y) { return keys[x] != keys[y] ? keys[x] > keys[y] : x < y; });
