@@ -268,18 +268,18 @@ RV_DEV void take_out(u32x4 (&vh)[ND], u32x4 (&vl)[ND], int k0, int kend, const Q
 // ----------------------------------------------------------- bf16, many queries
 // S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMAs, operands as pairs of planes
 // hi = bf16(x), lo = bf16(x - hi), as the cache holds K and V: a pair is within
-// 2^-17 of x, and with lo lo dropped (2^-16 of a product) fp32 rows come out within
-// 5e-6 of the exact result (fp32 MFMAs would cost 2.6 times these products:
-// 153 against 1198 / 3 TFLOP/s in library products).  Three products each; queries given in bf16 have no lo
-// plane, two products.  Scores, statistics and sums are fp32.  8 waves of TPW 16-query tiles: every
-// K and V operand read from LDS serves TPW tiles, and with one LDS reads bound
-// the kernel (512 KiB a tile and CU against 3072 cycles of MFMA), so calls with
-// more than 128 queries take two.  The cache holds tiles in operand order (k_elem
-// / v_elem): a 64-key tile is four spans that go global -> LDS directly,
-// double-buffered.
+// 2^-17 of x, and with lo lo dropped (2^-16 of a product) fp32 rows come out
+// within 5e-6 of the exact result (fp32 MFMAs would cost 2.6 times these
+// products: 153 against 1198 / 3 TFLOP/s in library products).  Three products
+// each; queries given in bf16 have no lo plane, two products.  Scores, statistics
+// and sums are fp32.  8 waves of TPW 16-query tiles: every K and V operand read
+// from LDS serves TPW tiles, and with one LDS reads bound the kernel (512 KiB a
+// tile and CU, 4096 cycles, against 192 MFMAs of 16), so calls with more than 128
+// queries take two.  The cache holds tiles in operand order (k_elem / v_elem): a
+// 64-key tile is four spans that go global -> LDS directly, double-buffered.
 // Bound by the matrix cores' power: 64 continuations of 32768 shared keys (70B
-// shape, fp32 rows) take 252 us with their own keys and the merge, 1.12 PFLOP/s of
-// products in the shared part, where a large library product reaches 1.20.  16
+// shape, fp32 rows) take 252 us with their own keys and the merge, 1.12 PFLOP/s
+// of products in the shared part, where a large library product reaches 1.20.  16
 // blocks of 31 rows over 2048 shared keys (8B) 67 us.
 template <int HD, int PART, int TPW, bool QLO>
 RV_DEV void attend_many(const ShareArgs& a, const Unit& u, uint16_t (&sm0)[4][kKB * HD], uint16_t (&sm1)[4][kKB * HD]) {
