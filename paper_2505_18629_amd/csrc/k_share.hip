@@ -269,7 +269,7 @@ RV_DEV void take_out(u32x4 (&vh)[ND], u32x4 (&vl)[ND], int k0, int kend, const Q
 // S^T = K Q^T and O^T += V^T P^T on 16x16x32 MFMAs, operands as pairs of planes
 // hi = bf16(x), lo = bf16(x - hi), as the cache holds K and V: a pair is within
 // 2^-17 of x, and with lo lo dropped (2^-16 of a product) fp32 rows come out
-// within 5e-6 of the exact result (fp32 MFMAs would cost 2.6 times these
+// within 6e-6 of the exact result (fp32 MFMAs would cost 2.6 times these
 // products: 153 against 1198 / 3 TFLOP/s in library products).  Three products
 // each; queries given in bf16 have no lo plane, two products.  Scores, statistics
 // and sums are fp32.  8 waves of TPW 16-query tiles: every K and V operand read
