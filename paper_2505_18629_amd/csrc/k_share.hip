@@ -21,7 +21,7 @@ enum { KIND_NONE = 0, KIND_FEW = 1, KIND_MANY = 2, KIND_MANY2 = 3, KIND_STREAM =
 // by queries q_begin.. of nq (query slots of one kv head).
 struct Unit {
   int seq, kbeg, kend, nq, q_begin, slot, kvh;
-  int first, rmax;  // shared part: the group's first member, rows per member
+  int first, rmax;  // shared part: the group's first member, and as in ShareArgs
   int pos0, row0;   // own part
 };
 
@@ -62,7 +62,7 @@ RV_DEV bool unit_of(const ShareArgs& a, int x, Unit& u) {
     u.first = a.first[i];
     u.rmax = a.rmax[i];
     u.seq = a.member[u.first];
-    u.nq = (a.first[i + 1] - u.first) * u.rmax * G;
+    u.nq = (u.rmax < 0 ? -u.rmax : (a.first[i + 1] - u.first) * u.rmax) * G;
     if (u.q_begin >= u.nq) return false;
     u.kbeg = run * sp.ks;
     u.kend = min(a.tiles[i] * kKB, u.kbeg + sp.ks);
@@ -81,6 +81,10 @@ RV_DEV Query query_of(const ShareArgs& a, const Unit& u, int q) {
     r.valid = q < u.nq;
     r.row = u.row0 + qc / G;
     r.last = u.pos0 + qc / G;
+  } else if (u.rmax < 0) {
+    r.valid = q < u.nq;
+    r.row = a.seq[u.seq].row0 + qc / G;
+    r.last = 0x7fffffff;
   } else {
     const int i = qc / G, m = i / u.rmax, seq = a.member[u.first + m];
     const int row0 = a.seq[seq].row0, n = a.seq[seq + 1].row0 - row0, k = i - m * u.rmax;

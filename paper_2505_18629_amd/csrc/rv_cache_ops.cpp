@@ -147,7 +147,7 @@ void plan_attend(const rv_cache* c, const int* pos0, const int* row0, ShareArgs&
     std::copy(p.member, p.member + c->B, a.member);
     std::copy(p.first, p.first + p.groups + 1, a.first);
     std::copy(p.tiles, p.tiles + p.groups, a.tiles);
-    std::copy(p.rmax, p.rmax + p.groups, a.rmax);
+    for (int g = 0; g < p.groups; ++g) a.rmax[g] = p.dense[g] ? -p.dense[g] : p.rmax[g];
   }
 }
 

@@ -322,7 +322,8 @@ struct ShareArgs {
   uint8_t member[RV_MAX_BATCH];
   uint8_t order[RV_MAX_BATCH];  // sequences by their own keys, most first
   int16_t first[kShareGroups + 1];
-  int32_t tiles[kShareGroups], rmax[kShareGroups];
+  int32_t tiles[kShareGroups];
+  int32_t rmax[kShareGroups];  // rows per member, or -(rows of all) where they follow each other
 };
 static_assert(sizeof(ShareArgs) <= 4096, "kernel arguments");
 // Every launch of one call: shared part, own part, merge.

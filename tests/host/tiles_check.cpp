@@ -269,7 +269,7 @@ static void programs() {
 // and every result has a place in the partial buffer.
 static void shares() {
   std::mt19937 r(11);
-  int grouped = 0;
+  int grouped = 0, dense = 0, strided = 0;
   for (int it = 0; it < 600; ++it) {
     const int B = 1 + r() % 40, max_len = 64 + r() % 3000, G = 1 + r() % 8, n_kv = 1 + r() % 3;
     TileOwners tl;
@@ -302,7 +302,17 @@ static void shares() {
     for (int g = 0; g < p.groups; ++g) {
       CHECK(p.first[g + 1] - p.first[g] >= 2 && p.tiles[g] >= 1);
       CHECK(p.tiles[g] * 64 <= p.sh.ks * p.sh.ns);
-      CHECK((p.first[g + 1] - p.first[g]) * p.rmax[g] * G <= p.sh.qpw * p.sh.nqg);
+      CHECK(p.slot_rows(g) * G <= p.sh.qpw * p.sh.nqg);
+      int rows = 0, next = row0[p.member[p.first[g]]];
+      bool follow = true;
+      for (int i = p.first[g]; i < p.first[g + 1]; ++i) {
+        const int b = p.member[i];
+        follow = follow && row0[b] == next;
+        next = row0[b + 1];
+        rows += row0[b + 1] - row0[b];
+      }
+      CHECK(p.dense[g] == (follow ? rows : 0));
+      (follow ? dense : strided) += 1;
       for (int i = p.first[g]; i < p.first[g + 1]; ++i) {
         const int b = p.member[i];
         CHECK(p.group_of[b] == g && !seen[b]++);
@@ -319,7 +329,7 @@ static void shares() {
       CHECK(pos[b] + n - k0 <= p.own.ks * p.own.ns);  // the merge's last run exists
     }
   }
-  CHECK(grouped > 200);
+  CHECK(grouped > 200 && dense > 20 && strided > 20);
 }
 
 // Many sequences: the order of the own part's workgroups names each once, most keys first.
